@@ -253,6 +253,136 @@ dbt_status dbt_op_gemm_tc_static(const void *W_dev, const void *X_dev, int32_t n
                                  int32_t force_split, float *Y_dev, int32_t *status_dev, void *cuda_stream,
                                  int32_t *split_used);
 
+/* ---- Operators for sampled and drafted tokens -------------------------------------------------------------------
+ * The paper's decode step takes one token per sequence and picks the likeliest (reading of Section 4.4).  The entries
+ * below serve programs that draw tokens, and programs that verify several drafted tokens per sequence in one pass over
+ * the weights: rotary positions (plain, or with the keys and values written into the cache's pages), attention of a tree
+ * of drafted tokens over the paged cache, sampling, and the acceptance of one branch of the tree.
+ *
+ * Common rules.
+ *  - All pointers are DEVICE unless marked; the device that they are on must be the current one; work is enqueued on
+ *    cuda_stream (a stream of that device) and nothing waits.  No call allocates memory, keeps state or uses memory that
+ *    another call uses too, beyond the caller's own buffers: calls on different streams may overlap as long as their
+ *    output, workspace and status buffers differ.  All calls may be captured into CUDA graphs.
+ *  - dtype is DBT_DTYPE_*: the type of activations and of the cache.  head strides and the like count elements.
+ *  - A cache layer is [2 (K,V)][num_pages][n_kv_heads][16][head_dim] -- one layer of the handle's pool --, 16-byte aligned,
+ *    head_dim 64 or 128; page_table int32 [B][pages_per_seq] with position t of sequence b in page table[b][t / 16],
+ *    slot t % 16.  Unlike a handle's own table it lives on the device.
+ *  - seq_lens int32 [B]: cached positions of each sequence, before its drafted nodes.  The nodes 0..n-1 of sequence b have
+ *    their keys and values at positions seq_lens[b] .. seq_lens[b] + n - 1.  node_counts int32 [B], or NULL: n_b nodes of
+ *    sequence b count (0..max_nodes; other values are clamped); NULL: all max_nodes.  What belongs to nodes behind n_b is
+ *    neither read nor written.  max_nodes is at most 64.
+ *  - parents int32 [B][max_nodes]: the parent of each node, less than the node's own number, or -1 (a root).
+ *  - status_dev int32 [2], zeroed by the caller: errors that only the device sees, {code, detail} as dbt_sync_status
+ *    reports them (2 = a page id out of range, or a position behind the table's last page, detail -1; 3 = a bounded wait
+ *    ran out; 4 = a parent that is not below its node, detail = the parent).  The first one stays.  Accesses stay inside
+ *    the buffers: a bad page id is read as page 0 and not written, a bad parent counts as -1.
+ *  - A message for a refused call is in dbt_last_error(NULL) of the calling thread. */
+
+/* Frequencies (angle per position) of the rot_dim / 2 rotated pairs, HOST double [rot_dim / 2], and the factor on rotated
+ * queries and keys, HOST (1 where the kind has none).  base_i = base^(-2 i / rot_dim). */
+enum {
+    DBT_ROPE_PLAIN = 0,  /* base_i */
+    DBT_ROPE_LINEAR = 1, /* base_i / factor: positions squeezed into the trained range */
+    DBT_ROPE_BASE = 2,   /* base * factor^(rot_dim / (rot_dim - 2)) for base: the slowest pair slows by factor, the fastest keeps */
+    DBT_ROPE_RAMP = 3,   /* pairs of at most `low` turns over trained_len slow by factor, of at least `high` turns keep, a linear ramp
+                            over the pairs between; the factor on queries and keys is 0.1 ln(factor) + 1 */
+    DBT_ROPE_BANDS = 4   /* by the turns over trained_len: up to `low` slow by factor, from `high` on keep, between them a blend
+                            linear in the turns */
+};
+typedef struct {
+    uint32_t struct_size; /* sizeof(dbt_rope_spec) */
+    int32_t kind;         /* DBT_ROPE_* */
+    int32_t rot_dim;      /* rotated elements of a head: even, >= 2 */
+    int32_t reserved;     /* 0 */
+    double base;          /* > 1 */
+    double factor;        /* >= 1 (all kinds but PLAIN) */
+    double trained_len;   /* > 0 (RAMP, BANDS) */
+    double low, high;     /* 0 < low < high (RAMP, BANDS) */
+} dbt_rope_spec;
+dbt_status dbt_rope_frequencies(const dbt_rope_spec *spec_host, double *freq_host, float *scale_host);
+
+/* Rotary positions: y = scale * R(position) x on the first rot_dim elements of every head, the others copied.
+ * x, y [rows][heads][head_dim], head_dim contiguous, with strides between rows and heads; y may be x with the same
+ * strides, else the two do not overlap.  positions int32 [rows]; freq double [rot_dim / 2] (dbt_rope_frequencies, on the
+ * device); angles are formed and reduced in 64 bits.  interleaved 0: pairs (i, i + rot_dim / 2); 1: pairs (2i, 2i + 1).
+ * inverse 1: the transposed map, R(-position) with the same scale, which is the gradient with respect to x. */
+dbt_status dbt_op_rope(const void *x, void *y, const int32_t *positions, const double *freq, int64_t rows, int32_t heads,
+                       int32_t head_dim, int32_t rot_dim, int64_t x_row_stride, int64_t x_head_stride, int64_t y_row_stride,
+                       int64_t y_head_stride, float scale, int32_t interleaved, int32_t inverse, int32_t dtype,
+                       void *cuda_stream);
+
+/* A step's queries and keys of drafted nodes rotated by positions int32 [B][max_nodes], the queries written to q_out
+ * [B][max_nodes][n_q_heads][head_dim] (contiguous; not q), the keys and values to the cache positions of their nodes.
+ * q, k, v [B][max_nodes][heads][head_dim], head_dim contiguous, strides for batch, node and head. */
+typedef struct {
+    uint32_t struct_size; /* sizeof(dbt_rope_append_args) */
+    int32_t dtype, B, max_nodes, n_q_heads, n_kv_heads, head_dim, rot_dim, interleaved;
+    int32_t num_pages, pages_per_seq;
+    float scale;
+    const void *q, *k, *v;
+    int64_t q_stride[3], k_stride[3], v_stride[3]; /* batch, node, head */
+    void *q_out, *cache_layer;
+    const int32_t *positions, *page_table, *seq_lens, *node_counts;
+    const double *freq;
+    int32_t *status_dev;
+} dbt_rope_append_args;
+dbt_status dbt_op_rope_append(const dbt_rope_append_args *args_host, void *cuda_stream);
+
+/* Attention of drafted nodes: node i of sequence b attends to the cached positions 0 .. seq_lens[b]-1 and, among the nodes,
+ * to itself and its ancestors.  q [B][max_nodes][n_q_heads][head_dim] with strides (head_dim contiguous), out
+ * [B][max_nodes][n_q_heads][head_dim] contiguous, query head h reads KV head h / (n_q_heads / n_kv_heads); scores are
+ * multiplied by softmax_scale (0: 1 / sqrt(head_dim)).  Softmax in fp32.  workspace: dbt_op_attn_tree_workspace bytes,
+ * 256-byte aligned, nothing in it needs to be initialised. */
+typedef struct {
+    uint32_t struct_size; /* sizeof(dbt_attn_tree_args) */
+    int32_t dtype, B, max_nodes, n_q_heads, n_kv_heads, head_dim;
+    int32_t num_pages, pages_per_seq;
+    float softmax_scale;
+    const void *q, *cache_layer;
+    int64_t q_stride[3]; /* batch, node, head */
+    void *out;
+    const int32_t *page_table, *seq_lens, *node_counts, *parents;
+    void *workspace;
+    size_t workspace_bytes;
+    int32_t *status_dev;
+} dbt_attn_tree_args;
+/* Bytes of workspace that this call needs (pointers are not looked at). */
+dbt_status dbt_op_attn_tree_workspace(const dbt_attn_tree_args *args_host, size_t *bytes_host);
+dbt_status dbt_op_attn_tree(const dbt_attn_tree_args *args_host, void *cuda_stream);
+
+/* A token per row of logits [rows][vocab] (DBT_DTYPE_*, row_stride elements apart), from one number u in [0, 1) a row
+ * (uniforms fp32 [rows]).  With w_i = exp((z_i - max z) / temperature):
+ *   top_k  > 0: the k largest logits stay (ties: the lower token id);
+ *   top_p  < 1: of those, in falling order, the shortest run that holds at least top_p of their mass;
+ *   min_p  > 0: of those the ones with w_i >= min_p.
+ * The likeliest token always stays.  The token is the first, in rising order of ids, at which the running sum of the
+ * remaining w exceeds u times their total.  temperature <= 0: the largest logit.  NaN logits count as -inf; a row without
+ * any logit above -inf gives token -1 and log-probability -inf; where the largest is +inf, the infinite ones share all mass.
+ * temperature, top_p, min_p fp32 [rows], top_k int32 [rows]; each may be NULL (1, off, off, off).  tokens int32 [rows];
+ * logprobs fp32 [rows] or NULL: log of the token's share of the remaining mass (0 where the temperature is <= 0).
+ * Masses are formed and summed in 64 bits.  2 <= vocab <= 262144. */
+dbt_status dbt_op_sample(const void *logits, int32_t dtype, int32_t rows, int32_t vocab, int64_t row_stride,
+                         const float *uniforms, const float *temperature, const int32_t *top_k, const float *top_p,
+                         const float *min_p, int32_t *tokens, float *logprobs, void *cuda_stream);
+
+/* Acceptance: from node 0 on, the walk goes to the child (lowest number first) whose token is the one sampled at the
+ * current node, as long as there is one.  tokens, parents, sampled int32 [B][max_nodes].  Outputs: path int32
+ * [B][max_nodes], the accepted nodes in order (node 0 first), -1 behind them; counts int32 [B]; next_tokens int32 [B], the
+ * token sampled at the last accepted node (-1 for a sequence without nodes); new_lens int32 [B], seq_lens + count (a buffer
+ * of its own, not seq_lens).  The accepted nodes' keys and values are moved to positions seq_lens[b] .. + count - 1 in all n_layers
+ * layers of pool [n_layers][2][num_pages][n_kv_heads][16][head_dim]; the positions behind keep what they hold. */
+typedef struct {
+    uint32_t struct_size; /* sizeof(dbt_tree_accept_args) */
+    int32_t dtype, B, max_nodes, n_layers, n_kv_heads, head_dim;
+    int32_t num_pages, pages_per_seq;
+    const int32_t *tokens, *parents, *sampled, *page_table, *seq_lens, *node_counts;
+    void *pool;
+    int32_t *path, *counts, *next_tokens, *new_lens;
+    int32_t *status_dev;
+} dbt_tree_accept_args;
+dbt_status dbt_op_tree_accept(const dbt_tree_accept_args *args_host, void *cuda_stream);
+
 /* Per-kernel timing for the roofline report (paper Eq. roofline, Eq. decode_traffic: time
  * against the bytes that must move).  Between begin and end every kernel launch is bracketed
  * by CUDA events on the handle's stream; end waits for the stream and sums, per kernel family,

@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 
 import torch
 
@@ -24,7 +25,9 @@ EXPORTS = ["dbt_query_sizes", "dbt_create", "dbt_destroy", "dbt_set_page_table",
            "dbt_seq_len", "dbt_prefill", "dbt_decode_step", "dbt_decode_step_primary_only", "dbt_decode_step_host",
            "dbt_decode_step_primary_only_host", "dbt_last_experts", "dbt_last_expert_union", "dbt_sync_status",
            "dbt_launch_count", "dbt_last_error", "dbt_version", "dbt_profile_begin", "dbt_profile_end", "dbt_op_gemm_tc",
-           "dbt_op_gemm_tc_static", "dbt_kv_export", "dbt_kv_import", "dbt_prefill_boundary"]
+           "dbt_op_gemm_tc_static", "dbt_kv_export", "dbt_kv_import", "dbt_prefill_boundary", "dbt_rope_frequencies",
+           "dbt_op_rope", "dbt_op_rope_append", "dbt_op_attn_tree_workspace", "dbt_op_attn_tree", "dbt_op_sample",
+           "dbt_op_tree_accept"]
 
 
 class DbtError(RuntimeError):
@@ -95,6 +98,14 @@ def load_library():
     L.dbt_kv_import.argtypes = [vp, vp, i32, i32, vp, vp]
     L.dbt_op_gemm_tc.argtypes = [vp, vp, i32, i32, i32, i32, vp, vp, C.c_size_t, vp, vp, i32p]
     L.dbt_op_gemm_tc_static.argtypes = [vp, vp, i32, i32, i32, i32, vp, vp, vp, i32p]
+    L.dbt_rope_frequencies.argtypes = [vp, vp, vp]
+    L.dbt_op_rope.argtypes = [vp, vp, vp, vp, C.c_int64, i32, i32, i32, C.c_int64, C.c_int64, C.c_int64, C.c_int64, C.c_float, i32,
+                              i32, i32, vp]
+    L.dbt_op_rope_append.argtypes = [vp, vp]
+    L.dbt_op_attn_tree_workspace.argtypes = [vp, C.POINTER(C.c_size_t)]
+    L.dbt_op_attn_tree.argtypes = [vp, vp]
+    L.dbt_op_sample.argtypes = [vp, i32, i32, i32, C.c_int64, vp, vp, vp, vp, vp, vp, vp, vp]
+    L.dbt_op_tree_accept.argtypes = [vp, vp]
     L.dbt_profile_begin.argtypes = [vp]
     L.dbt_profile_end.argtypes = [vp, C.POINTER(DbtProfileEntry), i32, i32p]
     L.dbt_launch_count.argtypes = [vp]
@@ -177,6 +188,244 @@ def op_gemm_tc_static(W: torch.Tensor, X: torch.Tensor, force_split: int = 0, Y:
     if code[0] != 0:  # 3: a bounded device wait ran out (the codes of dbt_sync_status)
         raise DbtError(7 if code[0] == 3 else 6, f"device status {code}")
     return Y, used.value
+
+
+# ---- operators for sampled and drafted tokens -----------------------------------------------------------------------
+# The argument structures of include/dbt.h as `struct` formats (native alignment): packing one costs a microsecond, filling a
+# ctypes structure several.
+ROPE_SPEC_FORMAT = struct.Struct("@I3i5d")
+ROPE_APPEND_FORMAT = struct.Struct("@I10if3P9q2P4PPP")
+ATTN_TREE_FORMAT = struct.Struct("@I8if2P3qP4PPNP")
+TREE_ACCEPT_FORMAT = struct.Struct("@I8i6PP4PP")
+ROPE_KINDS = {"plain": 0, "linear": 1, "base": 2, "ramp": 3, "bands": 4}
+_DTYPES = {torch.float32: 0, torch.bfloat16: 1}
+
+
+def _need(cond, message: str):
+    if not cond:
+        raise DbtError(1, message)
+
+
+def _dtype(t: torch.Tensor) -> int:
+    _need(t.dtype in _DTYPES, f"float32 or bfloat16 expected, got {t.dtype}")
+    return _DTYPES[t.dtype]
+
+
+def _ints(name: str, t, shape):
+    """An int32 tensor of that shape, contiguous (None passes)."""
+    if t is not None:
+        _need(t.dtype is torch.int32 and t.shape == shape and t.is_contiguous(), f"{name}: contiguous int32 {tuple(shape)} expected")
+
+
+def _enqueue(fn, tensors, *args):
+    """Call the entry on the current stream of the device that all tensors are on."""
+    dev = tensors[0].get_device()
+    for t in tensors:
+        if t is not None and t.get_device() != dev:
+            raise DbtError(1, "all tensors have to be on one GPU")
+    _need(dev >= 0, "the tensors have to be on a GPU")
+    if dev == torch._C._cuda_getDevice():
+        st = fn(*args, torch._C._cuda_getCurrentRawStream(dev))
+    else:
+        with torch.cuda.device(dev):
+            st = fn(*args, torch._C._cuda_getCurrentRawStream(dev))
+    if st != DBT_OK:
+        raise DbtError(st, load_library().dbt_last_error(None).decode())
+
+
+def check_status(status: torch.Tensor):
+    """Wait for a status word that operators were given, and raise what they recorded in it."""
+    code = status.cpu().tolist()
+    if code[0] != 0:
+        raise DbtError(7 if code[0] == 3 else 6, f"device status {code}")
+
+
+def _enqueue_checked(fn, tensors, status, pack):
+    """With a caller's status word the call does not wait; without one it waits and raises what the device found."""
+    own = status is None
+    if own:
+        status = torch.zeros(2, dtype=torch.int32, device=tensors[0].device)
+    else:
+        _ints("status", status, (2,))
+    _enqueue(fn, (*tensors, status), pack(status.data_ptr()))
+    if own:
+        check_status(status)
+
+
+def rope_frequencies(rot_dim: int, base: float = 10000.0, kind: str = "plain", factor: float = 1.0, trained_len: float = 0.0,
+                     low: float = 1.0, high: float = 32.0) -> tuple[torch.Tensor, float]:
+    """(angle per position of each of the rot_dim / 2 pairs, float64 on the CPU; factor on queries and keys) for
+    contexts as trained ("plain") or longer: "linear", "base", "ramp", "bands" as include/dbt.h defines them."""
+    L = load_library()
+    _need(kind in ROPE_KINDS, f"kind: one of {sorted(ROPE_KINDS)}")
+    freq = torch.empty(max(rot_dim // 2, 1), dtype=torch.float64)
+    scale = C.c_float(1.0)
+    spec = ROPE_SPEC_FORMAT.pack(ROPE_SPEC_FORMAT.size, ROPE_KINDS[kind], rot_dim, 0, base, factor, trained_len, low, high)
+    st = L.dbt_rope_frequencies(spec, freq.data_ptr(), C.addressof(scale))
+    if st != DBT_OK:
+        raise DbtError(st, L.dbt_last_error(None).decode())
+    return freq, scale.value
+
+
+def op_rope(x: torch.Tensor, positions: torch.Tensor, freq: torch.Tensor, scale: float = 1.0, interleaved: bool = False,
+            inverse: bool = False, out: torch.Tensor | None = None) -> torch.Tensor:
+    """x [rows, heads, head_dim] with the first 2 * freq.numel() elements of every head rotated by positions [rows] (int32)
+    times freq (float64, on x's device).  inverse: the transposed map, which is the gradient.  out may be x."""
+    L = load_library()
+    dt = _dtype(x)
+    _need(x.dim() == 3 and x.stride(2) == 1, "x: [rows, heads, head_dim] with contiguous head_dim expected")
+    rows, heads, dim = x.shape
+    if out is None:
+        out = torch.empty((rows, heads, dim), dtype=x.dtype, device=x.device)
+    _need(out.shape == x.shape and out.dtype is x.dtype and out.stride(2) == 1, "out: x's shape and type, contiguous head_dim")
+    _ints("positions", positions, (rows,))
+    _need(freq.dtype is torch.float64 and freq.dim() == 1 and freq.is_contiguous(), "freq: contiguous float64 [rot_dim / 2] expected")
+    _enqueue(L.dbt_op_rope, (x, out, positions, freq), x.data_ptr(), out.data_ptr(), positions.data_ptr(), freq.data_ptr(), rows, heads,
+             dim, 2 * freq.numel(), x.stride(0), x.stride(1), out.stride(0), out.stride(1), scale, int(interleaved), int(inverse), dt)
+    return out
+
+
+def _cache_shape(cache: torch.Tensor, dims: int, dtype):
+    _need(cache.dim() == dims and cache.shape[-5] == 2 and cache.shape[-2] == 16 and cache.is_contiguous() and cache.dtype is dtype,
+          "cache: contiguous [.., 2, pages, kv heads, 16, head_dim] of the activations' type expected")
+    return cache.shape[-4], cache.shape[-3], cache.shape[-1]
+
+
+def _heads(name: str, t: torch.Tensor, B: int, N: int, dim: int, dtype):
+    _need(t.dim() == 4 and t.shape[0] == B and t.shape[1] == N and t.shape[3] == dim and t.stride(3) == 1 and t.dtype is dtype,
+          f"{name}: [B, nodes, heads, head_dim] of the cache's type with contiguous head_dim expected")
+
+
+def op_rope_append(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, positions: torch.Tensor, freq: torch.Tensor, cache_layer: torch.Tensor,
+                   page_table: torch.Tensor, seq_lens: torch.Tensor, counts: torch.Tensor | None = None, scale: float = 1.0,
+                   interleaved: bool = False, out: torch.Tensor | None = None, status: torch.Tensor | None = None) -> torch.Tensor:
+    """q [B, N, query heads, head_dim], k, v [B, N, kv heads, head_dim] (any strides but the last) of N nodes per sequence: q and k
+    rotated by positions [B, N]; the keys and values go to cache positions seq_lens[b] + node of cache_layer [2, pages, kv heads, 16,
+    head_dim], the rotated queries are returned.  counts [B]: nodes that count; rows behind them are left as they were."""
+    L = load_library()
+    dt = _dtype(q)
+    pages, nkv, dim = _cache_shape(cache_layer, 5, q.dtype)
+    _need(q.dim() == 4, "q: [B, nodes, heads, head_dim] expected")
+    B, N, nq, _ = q.shape
+    _heads("q", q, B, N, dim, q.dtype)
+    _heads("k", k, B, N, dim, q.dtype)
+    _heads("v", v, B, N, dim, q.dtype)
+    _need(k.shape[2] == nkv and v.shape[2] == nkv, "k, v: the cache's number of heads expected")
+    if out is None:
+        out = torch.empty((B, N, nq, dim), dtype=q.dtype, device=q.device)
+    _need(out.shape == q.shape and out.dtype is q.dtype and out.is_contiguous(), "out: contiguous, q's shape and type")
+    _need(page_table.dim() == 2, "page_table: [B, pages per sequence] expected")
+    _ints("positions", positions, (B, N))
+    _ints("page_table", page_table, (B, page_table.shape[1]))
+    _ints("seq_lens", seq_lens, (B,))
+    _ints("counts", counts, (B,))
+    _need(freq.dtype is torch.float64 and freq.dim() == 1 and freq.is_contiguous(), "freq: contiguous float64 [rot_dim / 2] expected")
+
+    def pack(status_ptr):
+        return ROPE_APPEND_FORMAT.pack(
+            ROPE_APPEND_FORMAT.size, dt, B, N, nq, nkv, dim, 2 * freq.numel(), int(interleaved), pages, page_table.shape[1], scale,
+            q.data_ptr(), k.data_ptr(), v.data_ptr(), *q.stride()[:3], *k.stride()[:3], *v.stride()[:3], out.data_ptr(),
+            cache_layer.data_ptr(), positions.data_ptr(), page_table.data_ptr(), seq_lens.data_ptr(),
+            0 if counts is None else counts.data_ptr(), freq.data_ptr(), status_ptr)
+
+    _enqueue_checked(L.dbt_op_rope_append, (q, k, v, out, cache_layer, positions, page_table, seq_lens, counts, freq), status, pack)
+    return out
+
+
+def op_attn_tree(q: torch.Tensor, cache_layer: torch.Tensor, page_table: torch.Tensor, seq_lens: torch.Tensor, parents: torch.Tensor,
+                 counts: torch.Tensor | None = None, softmax_scale: float = 0.0, out: torch.Tensor | None = None,
+                 workspace: torch.Tensor | None = None, status: torch.Tensor | None = None) -> torch.Tensor:
+    """Attention of the N drafted nodes of every sequence: q [B, N, query heads, head_dim]; node i sees the seq_lens[b] cached positions,
+    itself and its ancestors by parents [B, N] (-1: a root), whose keys and values stand in the cache behind them.  workspace (uint8, at
+    least attn_tree_workspace(...) bytes) is allocated when none is given."""
+    L = load_library()
+    dt = _dtype(q)
+    pages, nkv, dim = _cache_shape(cache_layer, 5, q.dtype)
+    _need(q.dim() == 4, "q: [B, nodes, heads, head_dim] expected")
+    B, N, nq, _ = q.shape
+    _heads("q", q, B, N, dim, q.dtype)
+    if out is None:
+        out = torch.empty((B, N, nq, dim), dtype=q.dtype, device=q.device)
+    _need(out.shape == q.shape and out.dtype is q.dtype and out.is_contiguous(), "out: contiguous, q's shape and type")
+    _need(page_table.dim() == 2, "page_table: [B, pages per sequence] expected")
+    _ints("page_table", page_table, (B, page_table.shape[1]))
+    _ints("seq_lens", seq_lens, (B,))
+    _ints("parents", parents, (B, N))
+    _ints("counts", counts, (B,))
+    if workspace is None:
+        workspace = torch.empty(attn_tree_workspace(q, cache_layer, page_table), dtype=torch.uint8, device=q.device)
+    _need(workspace.is_contiguous(), "workspace: contiguous expected")
+
+    def pack(status_ptr):
+        return ATTN_TREE_FORMAT.pack(
+            ATTN_TREE_FORMAT.size, dt, B, N, nq, nkv, dim, pages, page_table.shape[1], softmax_scale, q.data_ptr(), cache_layer.data_ptr(),
+            *q.stride()[:3], out.data_ptr(), page_table.data_ptr(), seq_lens.data_ptr(), 0 if counts is None else counts.data_ptr(),
+            parents.data_ptr(), workspace.data_ptr(), workspace.numel() * workspace.element_size(), status_ptr)
+
+    _enqueue_checked(L.dbt_op_attn_tree, (q, out, cache_layer, page_table, seq_lens, parents, counts, workspace), status, pack)
+    return out
+
+
+def attn_tree_workspace(q: torch.Tensor, cache_layer: torch.Tensor, page_table: torch.Tensor) -> int:
+    """Bytes of workspace that op_attn_tree needs for tensors of these shapes."""
+    L = load_library()
+    B, N, nq, dim = q.shape
+    n = C.c_size_t(0)
+    args = ATTN_TREE_FORMAT.pack(ATTN_TREE_FORMAT.size, _dtype(q), B, N, nq, cache_layer.shape[2], dim, cache_layer.shape[1], page_table.shape[1],
+                                 0.0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0)
+    st = L.dbt_op_attn_tree_workspace(args, C.byref(n))
+    if st != DBT_OK:
+        raise DbtError(st, L.dbt_last_error(None).decode())
+    return n.value
+
+
+def op_sample(logits: torch.Tensor, uniforms: torch.Tensor, temperature: torch.Tensor | None = None, top_k: torch.Tensor | None = None,
+              top_p: torch.Tensor | None = None, min_p: torch.Tensor | None = None) -> tuple[torch.Tensor, torch.Tensor]:
+    """A token per row of logits [rows, vocab] from one number in [0, 1) a row (uniforms fp32 [rows]); temperature, top_p, min_p fp32 [rows]
+    and top_k int32 [rows], each optional.  Returns (tokens int32 [rows], log of each token's share of what the filters leave)."""
+    L = load_library()
+    dt = _dtype(logits)
+    _need(logits.dim() == 2 and logits.stride(1) == 1, "logits: [rows, vocab] with contiguous rows expected")
+    R, V = logits.shape
+    for name, t in (("uniforms", uniforms), ("temperature", temperature), ("top_p", top_p), ("min_p", min_p)):
+        if t is not None:
+            _need(t.dtype is torch.float32 and t.shape == (R,) and t.is_contiguous(), f"{name}: contiguous float32 [rows] expected")
+    _ints("top_k", top_k, (R,))
+    tokens = torch.empty(R, dtype=torch.int32, device=logits.device)
+    logprobs = torch.empty(R, dtype=torch.float32, device=logits.device)
+    _enqueue(L.dbt_op_sample, (logits, uniforms, temperature, top_k, top_p, min_p), logits.data_ptr(), dt, R, V,
+             logits.stride(0) if R > 1 else V, uniforms.data_ptr(), _p(temperature), _p(top_k), _p(top_p), _p(min_p), tokens.data_ptr(),
+             logprobs.data_ptr())
+    return tokens, logprobs
+
+
+def op_tree_accept(tokens: torch.Tensor, parents: torch.Tensor, sampled: torch.Tensor, pool: torch.Tensor, page_table: torch.Tensor,
+                   seq_lens: torch.Tensor, counts: torch.Tensor | None = None, status: torch.Tensor | None = None):
+    """The walk from node 0 along the children whose token was sampled at their parent; the accepted nodes' rows of pool [layers, 2, pages,
+    kv heads, 16, head_dim] are moved together behind the cached positions.  tokens, parents, sampled [B, N] int32.  Returns (path [B, N],
+    accepted nodes [B], token sampled at the last of them [B], new lengths [B]), all int32."""
+    L = load_library()
+    dt = _dtype(pool)
+    pages, nkv, dim = _cache_shape(pool, 6, pool.dtype)
+    _need(tokens.dim() == 2 and page_table.dim() == 2, "tokens: [B, nodes], page_table: [B, pages per sequence] expected")
+    B, N = tokens.shape
+    _ints("tokens", tokens, (B, N))
+    _ints("parents", parents, (B, N))
+    _ints("sampled", sampled, (B, N))
+    _ints("page_table", page_table, (B, page_table.shape[1]))
+    _ints("seq_lens", seq_lens, (B,))
+    _ints("counts", counts, (B,))
+    path = torch.empty((B, N), dtype=torch.int32, device=tokens.device)
+    accepted, following, lens = torch.empty((3, B), dtype=torch.int32, device=tokens.device).unbind(0)
+
+    def pack(status_ptr):
+        return TREE_ACCEPT_FORMAT.pack(
+            TREE_ACCEPT_FORMAT.size, dt, B, N, pool.shape[0], nkv, dim, pages, page_table.shape[1], tokens.data_ptr(), parents.data_ptr(),
+            sampled.data_ptr(), page_table.data_ptr(), seq_lens.data_ptr(), 0 if counts is None else counts.data_ptr(), pool.data_ptr(),
+            path.data_ptr(), accepted.data_ptr(), following.data_ptr(), lens.data_ptr(), status_ptr)
+
+    _enqueue_checked(L.dbt_op_tree_accept, (tokens, parents, sampled, pool, page_table, seq_lens, counts), status, pack)
+    return path, accepted, following, lens
 
 
 def weights_to_device(weights: dict, device="cuda") -> dict:

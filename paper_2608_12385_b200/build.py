@@ -8,7 +8,7 @@ import sys
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libdbt_b200.so")
-SOURCES = ["dbt_api.cu"]
+SOURCES = ["dbt_api.cu", "dbt_ops.cu"]
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
               "-Xcompiler", "-fPIC", "-shared", "--expt-relaxed-constexpr"]
 
@@ -28,10 +28,19 @@ def build(force: bool = False, verbose: bool = False) -> str:
     nvcc = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
     tmp = LIB + f".tmp{os.getpid()}"
     extra = os.environ.get("DBT_NVCC_EXTRA", "").split()  # experiment knobs (-D...), empty in normal builds
-    cmd = [nvcc, *NVCC_FLAGS, *extra, *(["-Xptxas", "-v"] if verbose else []), "-o", tmp,
-           *[os.path.join(CSRC, s) for s in SOURCES], "-lcuda"]
-    subprocess.run(cmd, check=True)
-    os.replace(tmp, LIB)
+    flags = [*NVCC_FLAGS, *extra, *(["-Xptxas", "-v"] if verbose else [])]
+    compile_flags = [f for f in flags if f != "-shared"]
+    objects = [f"{tmp}.{i}.o" for i in range(len(SOURCES))]
+    try:
+        jobs = [subprocess.Popen([nvcc, *compile_flags, "-c", "-o", o, os.path.join(CSRC, s)]) for s, o in zip(SOURCES, objects)]
+        for job, s in [(job, s) for job, s in zip(jobs, SOURCES) if job.wait() != 0]:
+            raise subprocess.CalledProcessError(job.returncode, f"nvcc {s}")
+        subprocess.run([nvcc, *flags, "-o", tmp, *objects, "-lcuda"], check=True)
+        os.replace(tmp, LIB)
+    finally:
+        for o in objects:
+            if os.path.exists(o):
+                os.remove(o)
     return LIB
 
 

@@ -23,6 +23,7 @@
 #include "dbt_gemm_persist.cuh"
 #include "dbt_gemm_prompt.cuh"
 #include "dbt_gemm_group.cuh"
+#include "dbt_host.h"
 #include "dbt_kernels.cuh"
 #include "dbt_small.cuh"
 
@@ -2280,6 +2281,19 @@ dbt_status check_step_rows(dbt_model *m, int B, int grouped) {
 }
 
 }  // namespace
+
+dbt_status dbt::op_error(dbt_status st, const char *fmt, ...) {
+    char buf[512];
+    va_list ap;
+    va_start(ap, fmt);
+    vsnprintf(buf, sizeof buf, fmt, ap);
+    va_end(ap);
+    try {
+        g_create_error = buf;
+    } catch (...) {  // (no memory for the text: the status alone)
+    }
+    return st;
+}
 
 // ---------------------------------------------------------------------------------------
 

@@ -11,7 +11,7 @@ namespace dbt {
 constexpr int kWarp = 32;
 
 // Device status word values (see dbt_sync_status).
-enum : int { kStatusOk = 0, kStatusBadToken = 1, kStatusBadPage = 2, kStatusWaitExpired = 3 };
+enum : int { kStatusOk = 0, kStatusBadToken = 1, kStatusBadPage = 2, kStatusWaitExpired = 3, kStatusBadTree = 4 };
 
 __device__ __forceinline__ void report(int *status, int code, int detail) {
     if (atomicCAS(status, 0, code) == 0) status[1] = detail;
