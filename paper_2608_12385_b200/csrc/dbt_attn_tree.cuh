@@ -4,8 +4,9 @@
 // times their values.  All rows of a sequence that share a KV head read the same keys, so a block takes up to kRows of them
 // (node-major: row = node * G + head within the group) and streams the keys once in tiles.
 //
-// Work split.  The tiles of all (sequence, KV head, row block) items stand in one line, and the line is cut into equal runs,
-// one per block: no block waits for the longest sequence, whatever the lengths.  An item inside one run is written out at
+// Work split.  The tiles of all (sequence, KV head, row block) items stand in one line, each item headed by `lead` empty units for
+// what it costs besides its tiles, and the line is cut into equal runs, one per block: no block waits for the longest
+// sequence, whatever the lengths.  An item inside one run is written out at
 // once; of an item that is cut, each run leaves its unnormalised output with its maximum and sum in the workspace, and a second
 // kernel joins them in the order of the keys (no atomics: results do not depend on timing).  Lengths are read on the
 // device, so a captured call serves later lengths.
@@ -24,6 +25,8 @@ struct TreeAttnParams {
     int *status;
     long long qs[3];
     int B, N, G, hkv, num_pages, pps, blocks;
+    int lead;       // empty units ahead of an item
+    int q_vectors;  // queries can be read in 16-byte vectors
     float scale_log2;  // softmax scale * log2(e)
 };
 
@@ -33,8 +36,8 @@ struct TreeSeq {
 // Cached positions and nodes of a sequence, cut to what the page table holds.
 __device__ __forceinline__ TreeSeq tree_seq(const TreeAttnParams &p, int b, bool tell = false) {
     TreeSeq s;
-    s.len = ld_mut(p.seq_lens + b);
-    s.n = p.node_counts ? max(0, min(ld_mut(p.node_counts + b), p.N)) : p.N;
+    s.len = p.seq_lens[b];
+    s.n = p.node_counts ? max(0, min(p.node_counts[b], p.N)) : p.N;
     const long long cap = (long long)p.pps * 16;
     if (s.n > 0 && (s.len < 0 || s.len + (long long)s.n > cap)) {
         if (tell) report(p.status, kStatusBadPage, -1);
@@ -43,14 +46,19 @@ __device__ __forceinline__ TreeSeq tree_seq(const TreeAttnParams &p, int b, bool
     }
     return s;
 }
-// Tiles of one item of sequence b, its row blocks.
+// The line of units.
 template <int ROWS, int KEYS>
 struct TreePlan {
     static __device__ __forceinline__ int tiles(const TreeSeq &s) { return s.n > 0 ? (s.len + s.n + KEYS - 1) / KEYS : 0; }
     static __device__ __forceinline__ int row_blocks(const TreeAttnParams &p, const TreeSeq &s) { return (s.n * p.G + ROWS - 1) / ROWS; }
     static __device__ __forceinline__ long long units(const TreeAttnParams &p, int b) {
         const TreeSeq s = tree_seq(p, b);
-        return (long long)tiles(s) * row_blocks(p, s) * p.hkv;
+        return s.n > 0 ? (long long)(tiles(s) + p.lead) * row_blocks(p, s) * p.hkv : 0;
+    }
+    static __device__ __forceinline__ long long warp_total(long long v) {
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+        return v;
     }
     // By a whole warp: all units, and of sequence `upto` those before it.
     static __device__ __forceinline__ long long total(const TreeAttnParams &p, int lane, int upto, long long *before) {
@@ -60,13 +68,8 @@ struct TreePlan {
             sum += u;
             if (b < upto) part += u;
         }
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) {
-            sum += __shfl_xor_sync(0xffffffffu, sum, o);
-            part += __shfl_xor_sync(0xffffffffu, part, o);
-        }
-        if (before) *before = part;
-        return sum;
+        if (before) *before = warp_total(part);
+        return warp_total(sum);
     }
     // By a whole warp: the sequence that unit `at` (< total) lies in, and the units before it.
     static __device__ __forceinline__ int locate(const TreeAttnParams &p, int lane, long long at, long long *before) {
@@ -94,50 +97,49 @@ struct TreePlan {
 // Walks the items of a block's run of units.
 template <int ROWS, int KEYS>
 struct TreeWalk {
-    long long at, end;  // next unit, end of the run
-    int b, rb, h;       // current item
+    using Plan = TreePlan<ROWS, KEYS>;
+    long long end, item0;  // end of the run; the current item's first unit
+    int b, rb, h;          // current item
     TreeSeq s;
     int tiles, t0, t1, slot;  // the item's tiles, those of this run, the workspace slot (-1: the whole item is here)
-    long long first;          // the run's first unit
-    long long item0;          // the current item's first unit
+    // False where the run holds no tile.
     __device__ __forceinline__ bool start(const TreeAttnParams &p, int lane) {
-        const long long all = TreePlan<ROWS, KEYS>::total(p, lane, 0, nullptr), per = TreePlan<ROWS, KEYS>::per_block(p, all);
-        first = at = (long long)blockIdx.x * per;
+        const long long all = Plan::total(p, lane, 0, nullptr), per = Plan::per_block(p, all), at = (long long)blockIdx.x * per;
         end = min(all, at + per);
         if (at >= end) return false;
         long long before;
-        b = TreePlan<ROWS, KEYS>::locate(p, lane, at, &before);
+        b = Plan::locate(p, lane, at, &before);
         s = tree_seq(p, b, true);
-        tiles = TreePlan<ROWS, KEYS>::tiles(s);
-        const int item = (int)((at - before) / tiles), rbs = TreePlan<ROWS, KEYS>::row_blocks(p, s);
+        tiles = Plan::tiles(s);
+        const int units = tiles + p.lead, item = (int)((at - before) / units), rbs = Plan::row_blocks(p, s);
         h = item / rbs;
         rb = item - h * rbs;
-        item0 = before + (long long)item * tiles;
-        place();
-        return true;
+        item0 = before + (long long)item * units;
+        return place(p, at) || next(p);
     }
-    __device__ __forceinline__ void place() {
-        t0 = (int)(at - item0);
-        t1 = (int)min((long long)tiles, end - item0);
+    // The tiles of the current item in the run's part of it, from unit `at` on.
+    __device__ __forceinline__ bool place(const TreeAttnParams &p, long long at) {
+        const long long first = item0 + p.lead;
+        t0 = (int)max(0ll, at - first);
+        t1 = (int)min((long long)tiles, end - first);
         // at most two items of a run are cut: the one it begins inside, the one it ends inside
         slot = t0 == 0 && t1 == tiles ? -1 : 2 * (int)blockIdx.x + (t0 == 0);
+        return t1 > t0;
     }
     __device__ __forceinline__ bool next(const TreeAttnParams &p) {
-        at = item0 + t1;
-        if (at >= end) return false;
-        item0 += tiles;
-        if (++rb == TreePlan<ROWS, KEYS>::row_blocks(p, s)) {
+        item0 += tiles + p.lead;
+        if (item0 >= end) return false;
+        if (++rb == Plan::row_blocks(p, s)) {
             rb = 0;
             if (++h == p.hkv) {
                 h = 0;
                 do {
                     s = tree_seq(p, ++b, true);
-                    tiles = TreePlan<ROWS, KEYS>::tiles(s);
+                    tiles = Plan::tiles(s);
                 } while (tiles == 0);
             }
         }
-        place();
-        return true;
+        return place(p, item0);  // (false: the run ends in the item's empty units)
     }
 };
 
@@ -327,6 +329,509 @@ __global__ void __launch_bounds__(256, TreeSimtCfg<D, RM>::kBlocksPerSm) attn_tr
     } while (w.next(p));
 }
 
+// ---- tensor-core form: bf16 --------------------------------------------------------------------------------------
+// Two groups of four softmax warps, a thread per row, alternate on the tensor cores: while one group turns its scores into
+// probabilities the products of the other run.  PAIR (more than 128 rows share a KV head): the groups own a 128-row tile each and
+// both see every tile of 128 keys.  Otherwise they share one row tile and take the key tiles in turn; the two outputs are
+// joined where they stand, in tensor memory.  Per key tile: S = Q K^T into tensor memory, P = exp2 of the scaled scores less the row's
+// maximum written back over S as bf16, O += P V with P from tensor memory.  O is rescaled only when a row's maximum has grown by
+// more than 2^8 (P stays below 2^8: the same relative error).  P is rounded to bf16 (2^-9 on average, relative), which the
+// tensor cores need; the sum adds the unrounded values.
+//
+// What bounds it: K and V from HBM up to some 128 rows (64 KB a key tile at head dimension 128: 1.5 us of an SM's share); at 256 rows
+// the tensor pipe, the exponentials and HBM take about as long as one another.
+//
+// Values that are not finite.  A node that a row does not see has probability 0, but 0 * NaN in the product is NaN.  So the
+// values of the nodes, once in shared memory, are looked through: elements that are not finite are replaced by 0 there, and
+// the rows that do see the node add them at the end.  Slots behind the last node are cleared the same way.
+//
+// Roles: warps 0..3, 4..7 softmax, 8 TMA, 9 MMA and tensor memory.  All waits are bounded.
+template <int DH, bool PAIR>
+struct TreeMmaCfg {
+    static constexpr int kRows = PAIR ? 256 : 128;
+    static constexpr int kKeys = 128;
+    static constexpr int kThreads = 320;
+    static constexpr int kHalves = DH / 64;
+    static constexpr int kTileBytes = 128 * DH * 2;  // 128 rows of queries, keys or values
+    static constexpr int kQTiles = PAIR ? 2 : 1;
+    static constexpr int kStages = DH == 128 ? (PAIR ? 2 : 3) : 5;
+    static constexpr int kSmemBytes = (kQTiles + 2 * kStages) * kTileBytes + 1024 + 256;
+    static constexpr int kTmemCols = 512;
+    static_assert(kSmemBytes + 1024 <= 227 * 1024, "shared memory of one SM");
+};
+constexpr float kTreeRescaleLog2 = 8.f;
+
+template <int DH, bool PAIR>
+__global__ void __launch_bounds__(320, 1) attn_tree_mma_kernel(const __grid_constant__ CUtensorMap tmKV, const TreeAttnParams p) {
+    using Cfg = TreeMmaCfg<DH, PAIR>;
+    constexpr int STAGES = Cfg::kStages, HALVES = Cfg::kHalves, KS = DH / 16, KEYS = Cfg::kKeys, ROWS = Cfg::kRows;
+    constexpr uint32_t kHalfBytes = 128 * 128;  // queries: 128 rows of one 64-column piece
+    constexpr uint32_t kGroup = HALVES * 1024;  // keys, values: 8 rows, their 64-column pieces one after the other
+    extern __shared__ uint8_t smem_raw[];
+    __shared__ int parents_s[2][64];
+    __shared__ unsigned long long bad_s;
+    __shared__ int failed_s;
+    const uint32_t raw = smem_u32(smem_raw);
+    const uint32_t q_s = (raw + 1023u) & ~1023u, k_s = q_s + Cfg::kQTiles * Cfg::kTileBytes, v_s = k_s + STAGES * Cfg::kTileBytes;
+    const uint32_t bars = v_s + STAGES * Cfg::kTileBytes;
+    auto k_full = [&](int s) { return bars + 8u * s; };
+    auto k_empty = [&](int s) { return bars + 8u * (STAGES + s); };
+    auto v_full = [&](int s) { return bars + 8u * (2 * STAGES + s); };
+    auto v_empty = [&](int s) { return bars + 8u * (3 * STAGES + s); };
+    auto q_full = [&](int i) { return bars + 8u * (4 * STAGES + i); };
+    auto s_full = [&](int i) { return bars + 8u * (4 * STAGES + 2 + i); };
+    auto p_full = [&](int i) { return bars + 8u * (4 * STAGES + 4 + i); };
+    auto o_full = [&](int i) { return bars + 8u * (4 * STAGES + 6 + i); };
+    uint32_t *tmem_holder = reinterpret_cast<uint32_t *>(smem_raw + (bars - raw) + 8 * (4 * STAGES + 8));
+    static_assert(8 * (4 * STAGES + 8) + 4 <= 256, "barrier area");
+
+    // the groups' maxima and sums, in the queries' place: both groups write them when all products of the item are done
+    float2(*stats_s)[128] = reinterpret_cast<float2(*)[128]>(smem_raw + (q_s - raw));
+
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    if (tid == 0) {
+        for (int s = 0; s < STAGES; s++) {
+            mbar_init(k_full(s), 1);
+            mbar_init(k_empty(s), 1);
+            mbar_init(v_full(s), 1);
+            mbar_init(v_empty(s), 1);
+        }
+        for (int i = 0; i < 2; i++) {
+            mbar_init(q_full(i), PAIR ? 4 : 8);
+            mbar_init(s_full(i), 1);
+            mbar_init(p_full(i), 4);
+            mbar_init(o_full(i), 2);  // the tensor cores are done; the nodes' values have been looked through
+        }
+        failed_s = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 9) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_holder)),
+                     "r"((uint32_t)Cfg::kTmemCols)
+                     : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    __syncthreads();
+    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    const uint32_t tmem = *tmem_holder;
+    auto t_s = [&](int i) { return tmem + 128u * i; };
+    auto t_o = [&](int i) { return tmem + 256u + (uint32_t)DH * i; };
+    pdl_launch_dependents();  // (the joining kernel waits for this one before it reads anything)
+
+    TreeWalk<ROWS, KEYS> w;
+    const bool work = w.start(p, lane);
+    bool ok = true;
+    if (work && warp == 8) {
+        // ---- TMA: lane l brings page l of the tile
+        if (lane == 0) tma_prefetch_desc(&tmKV);
+        const uint64_t once = l2_evict_first_policy();
+        const bool reread = p.N * p.G > ROWS;  // other row blocks read the same pages soon
+        const long long v_row0 = (long long)p.num_pages * p.hkv * 16;
+        int c = 0, nk = 0, nv = 0;  // tiles begun; tiles of keys, of values requested
+        do {
+            const int pages_total = (w.s.len + w.s.n + 15) >> 4;
+            const bool loads = lane < 8;
+            int page = loads && w.t0 * 8 + lane < pages_total ? tree_page(p, w.b, w.t0 * 8 + lane) : 0;
+            for (int t = w.t0; t < w.t1 && ok; t++, c++) {
+                const int s = c % STAGES, np = min(8, pages_total - t * 8);
+                const int row = (int)(((long long)page * p.hkv + w.h) * 2);  // in groups of 8 rows
+                const uint32_t off = s * Cfg::kTileBytes + lane * 2 * kGroup;
+                auto load = [&](uint32_t base, uint32_t bar, long long row0) {
+                    if (!(loads && lane < np)) return;
+                    const int at = (int)(row0 / 8) + row;
+                    if (reread) tma_load_4d(base + off, &tmKV, bar, 0, 0, 0, at);
+                    else tma_load_4d_hint(base + off, &tmKV, bar, 0, 0, 0, at, once);
+                };
+                const int nx = (t + 1) * 8 + lane;
+                const int next_page = loads && t + 1 < w.t1 && nx < pages_total ? tree_page(p, w.b, nx) : 0;
+                if (lane == 0) {
+                    if (c >= STAGES) ok = mbar_wait(k_empty(s), ((c / STAGES) - 1) & 1);
+                    if (ok) mbar_expect_tx(k_full(s), (uint32_t)np * HALVES * 2048);
+                }
+                ok = __shfl_sync(0xffffffffu, ok, 0);
+                if (ok) load(k_s, k_full(s), 0);
+                nk += ok;
+                if (lane == 0 && ok) {
+                    if (c >= STAGES) ok = mbar_wait(v_empty(s), ((c / STAGES) - 1) & 1);
+                    if (ok) mbar_expect_tx(v_full(s), (uint32_t)np * HALVES * 2048);
+                }
+                ok = __shfl_sync(0xffffffffu, ok, 0);
+                if (ok) load(v_s, v_full(s), v_row0);
+                nv += ok;
+                page = next_page;
+            }
+        } while (ok && w.next(p));
+        if (!ok && lane == 0) report(p.status, kStatusWaitExpired, 900);
+        // the last loads have landed before the block leaves, also where a wait ran out
+        if (lane == 0) {
+            for (int j = max(0, nk - STAGES); j < nk; j++) mbar_wait(k_full(j % STAGES), (j / STAGES) & 1, kWaitCycles / STAGES);
+            for (int j = max(0, nv - STAGES); j < nv; j++) mbar_wait(v_full(j % STAGES), (j / STAGES) & 1, kWaitCycles / STAGES);
+        }
+    } else if (work && warp == 9) {
+        // ---- MMA issuer (lane 0; the whole warp looks through the nodes' values)
+        constexpr uint32_t idesc_qk = umma_idesc(KEYS);
+        constexpr uint32_t idesc_pv = umma_idesc(DH) | (1u << 16);  // B is MN-major
+        auto wait = [&](uint32_t bar, int parity) {
+            bool r = true;
+            if (lane == 0) r = mbar_wait(bar, parity & 1);
+            r = __shfl_sync(0xffffffffu, r, 0);
+            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+            return r;
+        };
+        auto qk = [&](int i, int c) {
+            if (lane != 0) return;
+            const int s = c % STAGES;
+#pragma unroll
+            for (int k = 0; k < KS; k++) {
+                const int h = k >> 2;
+                umma_f16(t_s(i), umma_smem_desc(q_s + (PAIR ? i : 0) * Cfg::kTileBytes + h * kHalfBytes) + 2 * (k & 3),
+                         umma_smem_desc_groups(k_s + s * Cfg::kTileBytes + h * 1024, kGroup, 0) + 2 * (k & 3), idesc_qk, k != 0);
+            }
+            umma_commit(s_full(i));
+        };
+        auto pv = [&](int i, int c, bool add) {
+            if (lane != 0) return;
+            const uint64_t vd = umma_smem_desc_groups(v_s + (c % STAGES) * Cfg::kTileBytes, kGroup, 1024);
+#pragma unroll
+            for (int k = 0; k < KEYS / 16; k++) umma_f16_ts(t_o(i), t_s(i) + 8 * k, vd + (2 * kGroup >> 4) * k, idesc_pv, add || k != 0);
+        };
+        auto done = [&](int i) {
+            if (lane != 0) return;
+            umma_commit(o_full(i));
+            asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(o_full(i)) : "memory");
+        };
+        unsigned long long bad = 0;
+        // values of tile t in stage s: clears what lies behind the last node, takes out node values that are not finite
+        auto look = [&](int t, int s) {
+            const int key0 = t * KEYS, first = max(0, w.s.len - key0), keys = min(KEYS, w.s.len + w.s.n - key0);
+            if (first >= KEYS) return;
+            auto at = [&](int chunk) {  // address of the chunk-th 16 bytes of the rows (and pieces) in order
+                const int row = chunk / (8 * HALVES), rest = chunk - row * (8 * HALVES);
+                return v_s + s * Cfg::kTileBytes + (row >> 3) * kGroup + (rest >> 3) * 1024 + (row & 7) * 128 + (rest & 7) * 16;
+            };
+            for (int i = keys * 8 * HALVES + lane; i < KEYS * 8 * HALVES; i += 32)
+                asm volatile("st.shared.v4.b32 [%0], {%1,%1,%1,%1};" ::"r"(at(i)), "r"(0u) : "memory");
+            uint32_t any = 0;
+#pragma unroll 8
+            for (int i = first * 8 * HALVES + lane; i < keys * 8 * HALVES; i += 32) {
+                uint32_t x[4];
+                asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(x[0]), "=r"(x[1]), "=r"(x[2]), "=r"(x[3]) : "r"(at(i)));
+                // an exponent of ones carries into the sign's place when one is added to it (the sign itself masked off)
+#pragma unroll
+                for (int k = 0; k < 4; k++) any |= (x[k] & 0x7f807f80u) + 0x00800080u;
+            }
+            if (__any_sync(0xffffffffu, any & 0x80008000u)) {  // rare
+                for (int i = first * 8 * HALVES + lane; i - lane < keys * 8 * HALVES; i += 32) {
+                    const bool in = i < keys * 8 * HALVES;
+                    bool found = false;
+                    if (in) {
+                        uint32_t x[4];
+                        asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(x[0]), "=r"(x[1]), "=r"(x[2]), "=r"(x[3]) : "r"(at(i)));
+#pragma unroll
+                        for (int k = 0; k < 4; k++) {
+                            if ((x[k] & 0x7f80u) == 0x7f80u) x[k] &= 0xffff0000u, found = true;
+                            if ((x[k] & 0x7f800000u) == 0x7f800000u) x[k] &= 0xffffu, found = true;
+                        }
+                        if (found) asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(at(i)), "r"(x[0]), "r"(x[1]), "r"(x[2]), "r"(x[3]) : "memory");
+                    }
+                    for (unsigned m = __ballot_sync(0xffffffffu, found); m; m &= m - 1)
+                        bad |= 1ull << (key0 + (i - lane + __ffs(m) - 1) / (8 * HALVES) - w.s.len);
+                }
+            }
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            __syncwarp();
+        };
+        int c = 0, qn = 0, pn[2] = {0, 0};
+        do {
+            const int T = w.t1 - w.t0, rows = min(ROWS, w.s.n * p.G - w.rb * ROWS);
+            const int groups = PAIR ? (rows > 128 ? 2 : 1) : 1;  // PAIR: groups with rows
+            bad = 0;
+            // (PAIR: also a group without rows says that it is done with the item before)
+            for (int i = 0; i < (PAIR ? 2 : 1) && ok; i++) ok = wait(q_full(i), qn);
+            qn++;
+            if (PAIR) {
+                ok = ok && wait(k_full(c % STAGES), c / STAGES);
+                if (ok) {
+                    for (int i = 0; i < groups; i++) qk(i, c);
+                    if (lane == 0) umma_commit(k_empty(c % STAGES));
+                }
+                for (int t = 0; t < T && ok; t++, c++) {
+                    if (t + 1 < T) ok = wait(k_full((c + 1) % STAGES), (c + 1) / STAGES);
+                    ok = ok && wait(v_full(c % STAGES), c / STAGES);
+                    if (!ok) break;
+                    look(w.t0 + t, c % STAGES);
+                    for (int i = 0; i < groups && ok; i++) {
+                        ok = wait(p_full(i), pn[i]++);
+                        if (!ok) break;
+                        pv(i, c, t > 0);
+                        if (t + 1 < T) {
+                            qk(i, c + 1);
+                        } else {
+                            if (lane == 0) bad_s = bad;
+                            done(i);
+                        }
+                    }
+                    if (lane == 0 && ok) {
+                        umma_commit(v_empty(c % STAGES));
+                        if (t + 1 < T) umma_commit(k_empty((c + 1) % STAGES));
+                    }
+                }
+            } else {
+                for (int t = 0; t < min(2, T) && ok; t++) {
+                    ok = wait(k_full((c + t) % STAGES), (c + t) / STAGES);
+                    if (!ok) break;
+                    qk(t, c + t);
+                    if (lane == 0) umma_commit(k_empty((c + t) % STAGES));
+                }
+                for (int t = 0; t < T && ok; t++, c++) {
+                    const int i = t & 1;
+                    ok = wait(v_full(c % STAGES), c / STAGES);
+                    if (!ok) break;
+                    look(w.t0 + t, c % STAGES);
+                    ok = wait(p_full(i), pn[i]++);
+                    if (!ok) break;
+                    pv(i, c, t > 1);
+                    if (lane == 0) umma_commit(v_empty(c % STAGES));
+                    if (t + 2 < T) {
+                        ok = wait(k_full((c + 2) % STAGES), (c + 2) / STAGES);
+                        if (!ok) break;
+                        qk(i, c + 2);
+                        if (lane == 0) umma_commit(k_empty((c + 2) % STAGES));
+                    } else {
+                        if (lane == 0 && t == T - 1) bad_s = bad;
+                        done(i);
+                    }
+                }
+            }
+        } while (ok && w.next(p));
+        if (!ok && lane == 0) report(p.status, kStatusWaitExpired, 910);
+    } else if (work && warp < 8) {
+        // ---- softmax: thread = row
+        const int i = warp >> 2, r = tid & 127;
+        const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
+        const uint32_t ts = t_s(i) + lanes;
+        const __nv_bfloat16 *q = reinterpret_cast<const __nv_bfloat16 *>(p.q);
+        const float sc = p.scale_log2, grow = kTreeRescaleLog2 / sc;
+        int sn = 0, on_ = 0, other_on = 0;
+        do {
+            const int T = w.t1 - w.t0, tile0 = w.rb * ROWS + (PAIR ? i * 128 : 0), rows = min(128, w.s.n * p.G - tile0);
+            const int jobs = PAIR ? (rows > 0 ? T : 0) : (T + 1 - i) / 2;
+            const bool mine = r < rows, active = (r & ~31) < rows;
+            const bool nodes = w.t1 * KEYS > w.s.len;  // this run's part of the item reaches the nodes
+            int parent = -1;
+            if (nodes && r < w.s.n) parent = p.parents[(size_t)w.b * p.N + r];
+            // the queries: PAIR a tile per group, else all eight warps load the one tile
+            {
+                constexpr int CH = DH / 8, STEP = PAIR ? 128 : 256, LOADS = 128 * CH / STEP, BATCH = LOADS < 8 ? LOADS : 8;
+                const int first = PAIR ? r : tid;
+                for (int l0 = 0; (!PAIR || rows > 0) && l0 < LOADS; l0 += BATCH) {
+                    uint4 x[BATCH];
+#pragma unroll
+                    for (int l = 0; l < BATCH; l++) {
+                        const int idx = first + (l0 + l) * STEP, row = idx / CH, ch = idx - row * CH;
+                        x[l] = make_uint4(0, 0, 0, 0);
+                        if (row < rows) {
+                            const int node = (tile0 + row) / p.G, g = (tile0 + row) - node * p.G;
+                            const __nv_bfloat16 *src = q + w.b * p.qs[0] + node * p.qs[1] + (w.h * p.G + g) * p.qs[2] + ch * 8;
+                            if (p.q_vectors) {
+                                x[l] = __ldg(reinterpret_cast<const uint4 *>(src));
+                            } else {
+                                uint32_t y[4];
+#pragma unroll
+                                for (int k = 0; k < 4; k++)
+                                    y[k] = (uint32_t)__bfloat16_as_ushort(src[2 * k]) | ((uint32_t)__bfloat16_as_ushort(src[2 * k + 1]) << 16);
+                                x[l] = make_uint4(y[0], y[1], y[2], y[3]);
+                            }
+                        }
+                    }
+#pragma unroll
+                    for (int l = 0; l < BATCH; l++) {
+                        const int idx = first + (l0 + l) * STEP, row = idx / CH, ch = idx - row * CH;
+                        asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(q_s + (PAIR ? i : 0) * Cfg::kTileBytes + (ch >> 3) * kHalfBytes +
+                                                                                   row * 128 + (((ch & 7) ^ (row & 7)) << 4)),
+                                     "r"(x[l].x), "r"(x[l].y), "r"(x[l].z), "r"(x[l].w)
+                                     : "memory");
+                    }
+                }
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");  // (the output of the item before has been read)
+                __syncwarp();
+                if (lane == 0) asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(q_full(PAIR ? i : 0)) : "memory");
+            }
+            // the nodes that this row sees
+            unsigned long long seen = 0;
+            if (nodes) {
+                if (r < w.s.n && (parent >= r || parent < -1)) {
+                    report(p.status, kStatusBadTree, parent);
+                    parent = -1;
+                }
+                asm volatile("bar.sync %0, 128;" ::"r"(2 + i) : "memory");  // (the item before is done with the list)
+                if (r < w.s.n) parents_s[i][r] = parent;
+                asm volatile("bar.sync %0, 128;" ::"r"(2 + i) : "memory");
+                if (mine) seen = tree_ancestors(parents_s[i], (tile0 + r) / p.G);
+            }
+            float m_use = -INFINITY, l_run = 0.f;
+            for (int j = 0; j < jobs; j++) {
+                const int key0 = (w.t0 + (PAIR ? j : 2 * j + i)) * KEYS;
+                ok = mbar_wait(s_full(i), sn++ & 1);
+                ok = __all_sync(0xffffffffu, ok);
+                if (!ok) break;
+                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                if (active) {
+                    uint32_t v[128];
+#pragma unroll
+                    for (int c = 0; c < 4; c++) tmem_ld32_issue(ts + 32 * c, v + 32 * c);
+                    tmem_ld_wait();
+                    if (key0 + KEYS > w.s.len) {
+                        const int at = w.s.len - key0;  // column of node 0
+                        unsigned long long lo, hi;
+                        if (at >= 64) {
+                            lo = ~0ull;
+                            hi = (at > 64 ? ~0ull >> (128 - at) : 0ull) | (seen << (at - 64));
+                        } else if (at >= 0) {
+                            lo = (at > 0 ? ~0ull >> (64 - at) : 0ull) | (seen << at);
+                            hi = at > 0 ? seen >> (64 - at) : 0ull;
+                        } else {
+                            lo = at > -64 ? seen >> -at : 0ull;
+                            hi = 0ull;
+                        }
+                        const uint32_t word[4] = {(uint32_t)lo, (uint32_t)(lo >> 32), (uint32_t)hi, (uint32_t)(hi >> 32)};
+#pragma unroll
+                        for (int c = 0; c < 128; c++)
+                            if (!((word[c >> 5] >> (c & 31)) & 1)) v[c] = 0xff800000u;
+                    }
+                    float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+                    for (int c = 0; c < 128; c++) mx[c & 3] = fmaxf(mx[c & 3], __uint_as_float(v[c]));
+                    const float m_tile = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
+                    if (j == 0) {
+                        m_use = m_tile;
+                    } else if (__any_sync(0xffffffffu, m_tile > m_use + grow)) {
+                        // s_full was signalled after the products of the tile before: O is at rest
+                        const float m_new = fmaxf(m_use, m_tile), corr = m_new == m_use ? 1.f : ex2_approx((m_use - m_new) * sc);
+                        m_use = m_new;
+                        l_run *= corr;
+#pragma unroll 1
+                        for (int c = 0; c < DH; c += 32) {
+                            uint32_t o[32];
+                            tmem_ld32_issue(t_o(i) + lanes + c, o);
+                            tmem_ld_wait();
+#pragma unroll
+                            for (int k = 0; k < 32; k++) o[k] = __float_as_uint(__uint_as_float(o[k]) * corr);
+                            tmem_st32(t_o(i) + lanes + c, o);
+                        }
+                    }
+                    const float off = m_use == -INFINITY ? 0.f : -m_use * sc;  // (nothing seen so far: exp2 of -inf)
+                    float sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                    for (int h = 0; h < 2; h++) {
+                        uint32_t pk[32];
+#pragma unroll
+                        for (int c = 0; c < 32; c++) {
+                            const float a = ex2_approx(fmaf(__uint_as_float(v[h * 64 + 2 * c]), sc, off));
+                            const float e = ex2_approx(fmaf(__uint_as_float(v[h * 64 + 2 * c + 1]), sc, off));
+                            sum[(2 * c) & 3] += a;
+                            sum[(2 * c + 1) & 3] += e;
+                            pk[c] = pack_bf16(a, e);
+                        }
+                        tmem_st32(ts + 32 * h, pk);
+                    }
+                    l_run += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+                    tmem_st_wait();
+                }
+                asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+                __syncwarp();
+                if (lane == 0) asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(p_full(i)) : "memory");
+            }
+            // ---- the item's output, or this run's part of it
+            if (ok && jobs > 0) {
+                ok = mbar_wait(o_full(i), on_++ & 1);
+                ok = __all_sync(0xffffffffu, ok);
+            }
+            const bool two = !PAIR && T > 1;  // both groups hold a part
+            float f0 = 1.f, f1 = 0.f;         // weights of the two outputs
+            if (!PAIR) {
+                if (ok && (i == 0 ? T > 1 : true)) {  // the other group's output
+                    ok = mbar_wait(o_full(1 - i), other_on++ & 1);
+                    ok = __all_sync(0xffffffffu, ok);
+                }
+                stats_s[i][r] = make_float2(m_use, l_run);
+                if (!ok) failed_s = 1;
+                asm volatile("bar.sync 1, 256;" ::: "memory");
+                ok = ok && !*(volatile int *)&failed_s;
+                const float2 a = stats_s[0][r], b = stats_s[1][r];
+                const float m = two ? fmaxf(a.x, b.x) : a.x;
+                f0 = a.x == m ? 1.f : ex2_approx((a.x - m) * sc);
+                f1 = !two ? 0.f : b.x == m ? 1.f : ex2_approx((b.x - m) * sc);
+                m_use = m;
+                l_run = a.y * f0 + (two ? b.y * f1 : 0.f);
+            }
+            if (!ok) {
+                if (lane == 0) report(p.status, kStatusWaitExpired, 920 + warp);
+                if (!PAIR) asm volatile("bar.sync 1, 256;" ::: "memory");
+                break;
+            }
+            if (active && (!PAIR || jobs > 0)) {
+                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                const unsigned long long bad = mine ? *(volatile unsigned long long *)&bad_s & seen : 0ull;
+                const float inv = w.slot >= 0 ? 1.f : l_run == 0.f ? 0.f : 1.f / l_run;
+                f0 *= inv;
+                f1 *= inv;
+                const int node = (tile0 + r) / p.G, g = (tile0 + r) - node * p.G;
+                float *part = p.part + ((size_t)max(w.slot, 0) * ROWS + (PAIR ? i * 128 : 0) + r) * DH;
+                __nv_bfloat16 *out = reinterpret_cast<__nv_bfloat16 *>(p.out) + (((size_t)w.b * p.N + node) * p.hkv * p.G + w.h * p.G + g) * DH;
+                // PAIR: the group's own tile; else the groups write half of the columns each
+                constexpr int COLS = PAIR ? DH : DH / 2;
+                const int col0 = PAIR ? 0 : i * COLS;
+#pragma unroll 1
+                for (int c = col0; c < col0 + COLS; c += 32) {
+                    uint32_t o[32], o2[32];
+                    __syncwarp();
+                    tmem_ld32_issue(t_o(PAIR ? i : 0) + lanes + c, o);
+                    if (!PAIR && two) tmem_ld32_issue(t_o(1) + lanes + c, o2);
+                    tmem_ld_wait();
+                    if (!mine) continue;
+                    float x[32];
+#pragma unroll
+                    for (int k = 0; k < 32; k++) {
+                        x[k] = __uint_as_float(o[k]) * f0;
+                        if (!PAIR && two) x[k] += __uint_as_float(o2[k]) * f1;
+                    }
+                    for (unsigned long long m = bad; m; m &= m - 1) {  // rare: values that are not finite
+                        const int at = w.s.len + __ffsll(m) - 1;
+                        const __nv_bfloat16 *v = reinterpret_cast<const __nv_bfloat16 *>(p.cache) +
+                                                 ((((size_t)p.num_pages + tree_page(p, w.b, at >> 4)) * p.hkv + w.h) * 16 + (at & 15)) * DH + c;
+#pragma unroll
+                        for (int k = 0; k < 32; k++) {
+                            const float y = __bfloat162float(v[k]);
+                            if (!isfinite(y)) x[k] += y;
+                        }
+                    }
+                    if (w.slot >= 0) {
+#pragma unroll
+                        for (int k = 0; k < 32; k += 4) *reinterpret_cast<float4 *>(part + c + k) = make_float4(x[k], x[k + 1], x[k + 2], x[k + 3]);
+                    } else {
+#pragma unroll
+                        for (int k = 0; k < 32; k += 8)
+                            *reinterpret_cast<uint4 *>(out + c + k) = make_uint4(pack_bf16(x[k], x[k + 1]), pack_bf16(x[k + 2], x[k + 3]),
+                                                                                 pack_bf16(x[k + 4], x[k + 5]), pack_bf16(x[k + 6], x[k + 7]));
+                    }
+                }
+                if (w.slot >= 0 && mine && (PAIR || i == 0))
+                    p.stats[(size_t)w.slot * ROWS + (PAIR ? i * 128 : 0) + r] = make_float2(m_use * sc, l_run);
+            }
+            // both groups have read both outputs and the statistics before the next item's products and queries
+            if (!PAIR) asm volatile("bar.sync 1, 256;" ::: "memory");
+        } while (w.next(p));
+    }
+    __syncwarp();
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    __syncthreads();
+    if (warp == 9)
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"((uint32_t)Cfg::kTmemCols) : "memory");
+}
+
 // ---- joining the parts of items that were cut --------------------------------------------------------------------
 // A warp per output row, in the order of the keys.
 template <typename T, int D, int ROWS, int KEYS>
@@ -343,7 +848,7 @@ __global__ void __launch_bounds__(256) attn_tree_join_kernel(const TreeAttnParam
     long long before;
     const long long per = Plan::per_block(p, Plan::total(p, lane, b, &before));
     const int tiles = Plan::tiles(s), rb = row / ROWS, r = row - rb * ROWS;
-    const long long item0 = before + (long long)(h * Plan::row_blocks(p, s) + rb) * tiles;
+    const long long item0 = before + (long long)(h * Plan::row_blocks(p, s) + rb) * (tiles + p.lead) + p.lead;  // its first tile
     const int c0 = (int)(item0 / per), c1 = (int)((item0 + tiles - 1) / per);
     if (c0 == c1) return;
     auto slot = [&](int c) -> size_t { return (size_t)(2 * c + (c == c0)) * ROWS + r; };

@@ -118,15 +118,17 @@ bool strides_fit(const int64_t *s, int n, int dtype) {
 
 // ---- tree attention ----------------------------------------------------------------------------------------------
 struct TreeShape {
-    int rows, keys, blocks, per_sm;
+    int rows, keys, blocks, per_sm, lead;
 };
 // Blocks: as many as the device holds at once, no more than there can be tiles.
 TreeShape tree_shape(const dbt_attn_tree_args &a) {
     TreeShape s;
-    const int G = a.n_q_heads / a.n_kv_heads;
-    s.rows = a.max_nodes * G <= 16 ? 16 : 64;
-    s.keys = kTsKeys;
+    const int G = a.n_q_heads / a.n_kv_heads, rows = a.max_nodes * G;
+    const bool mma = a.dtype == DBT_DTYPE_BF16;
+    s.rows = mma ? (rows <= 128 ? 128 : 256) : (rows <= 16 ? 16 : 64);
+    s.keys = mma ? 128 : kTsKeys;
     s.per_sm = s.rows == 16 ? 2 : 1;
+    s.lead = mma ? 5 : 1;  // an item costs about as much as five (one) of its tiles besides them: 63 us without, 42 us at 4..6 (16 ragged sequences)
     const long long tiles = ((long long)a.pages_per_seq * 16 + s.keys - 1) / s.keys, rbs = (a.max_nodes * G + s.rows - 1) / s.rows;
     const long long most = tiles * rbs * a.n_kv_heads * a.B, fit = (long long)sm_count() * s.per_sm;
     s.blocks = (int)(most < fit ? most : fit);
@@ -161,6 +163,18 @@ cudaError_t tree_simt(const TreeAttnParams &p, void *stream) {
     if (e != cudaSuccess) return e;
     const long long warps = (long long)p.B * p.hkv * p.N * p.G;
     return launch(attn_tree_join_kernel<T, D, Cfg::kRows, kTsKeys>, dim3((unsigned)((warps + 7) / 8)), 256, 0, stream, 1, true, p);
+}
+
+template <int D, bool PAIR>
+cudaError_t tree_mma(const TreeAttnParams &p, void *stream) {
+    using Cfg = TreeMmaCfg<D, PAIR>;
+    CUtensorMap map;
+    if (!make_prompt_kv_map(&map, p.cache, (uint64_t)2 * p.num_pages * p.hkv * 16, D)) return cudaErrorInvalidValue;
+    cudaError_t e = allow_smem(attn_tree_mma_kernel<D, PAIR>, Cfg::kSmemBytes);
+    if (e == cudaSuccess) e = launch(attn_tree_mma_kernel<D, PAIR>, dim3(p.blocks), Cfg::kThreads, Cfg::kSmemBytes, stream, 1, false, map, p);
+    if (e != cudaSuccess) return e;
+    const long long warps = (long long)p.B * p.hkv * p.N * p.G;
+    return launch(attn_tree_join_kernel<__nv_bfloat16, D, Cfg::kRows, Cfg::kKeys>, dim3((unsigned)((warps + 7) / 8)), 256, 0, stream, 1, true, p);
 }
 
 }  // namespace
@@ -315,6 +329,8 @@ dbt_status dbt_op_attn_tree(const dbt_attn_tree_args *a, void *cuda_stream) {
     p.num_pages = a->num_pages;
     p.pps = a->pages_per_seq;
     p.blocks = s.blocks;
+    p.lead = s.lead;
+    p.q_vectors = aligned(a->q, 16) && strides_fit(a->q_stride, 3, a->dtype);
     p.scale_log2 = (a->softmax_scale > 0.f ? a->softmax_scale : 1.f / std::sqrt((float)a->head_dim)) * 1.4426950408889634f;
     cudaError_t e;
     const bool few = s.rows == 16, wide = a->head_dim == 128;
@@ -322,8 +338,8 @@ dbt_status dbt_op_attn_tree(const dbt_attn_tree_args *a, void *cuda_stream) {
         e = wide ? (few ? tree_simt<float, 128, 1>(p, cuda_stream) : tree_simt<float, 128, 4>(p, cuda_stream))
                  : (few ? tree_simt<float, 64, 1>(p, cuda_stream) : tree_simt<float, 64, 4>(p, cuda_stream));
     else
-        e = wide ? (few ? tree_simt<__nv_bfloat16, 128, 1>(p, cuda_stream) : tree_simt<__nv_bfloat16, 128, 4>(p, cuda_stream))
-                 : (few ? tree_simt<__nv_bfloat16, 64, 1>(p, cuda_stream) : tree_simt<__nv_bfloat16, 64, 4>(p, cuda_stream));
+        e = wide ? (s.rows == 128 ? tree_mma<128, false>(p, cuda_stream) : tree_mma<128, true>(p, cuda_stream))
+                 : (s.rows == 128 ? tree_mma<64, false>(p, cuda_stream) : tree_mma<64, true>(p, cuda_stream));
     return launched(e, "attn_tree");
 }
 
