@@ -4,21 +4,28 @@
 // count, top-p by mass, min-p by value; the kept set is the shortest of the three.  The token is the first one, in rising
 // order of ids, at which the running sum of the kept w exceeds u times their total.
 //
-// A row is held by the shared memory of a cluster of 1 to 8 blocks, so the logits are read from HBM once, whatever the
-// filters.  No row is sorted as a whole.  The border of a filter is found by narrowing: the row's values between two bounds
-// are dropped into 16 buckets (equal steps of the float's ordered bit pattern, the last one open below), the blocks add up
-// their counts and masses, and the bucket that holds the border is the next range.  As soon as what lies above the range and
-// in it is at most kSmList values -- mostly after one or two rounds -- the first block gathers these, sorts them and finishes alone.
-// Flat rows, whose kept set is larger, go on until the range itself is that short, or a single value; then one pass in
-// the order of ids sums what is kept.
+// A row is shared out over a cluster of 1 to 8 blocks.  Its logits come from HBM once and are read again, from L1 or L2, by the
+// passes that follow (held in shared memory they left room for two blocks per SM; as it is four are resident and cover one
+// another's barriers: 256 rows of 128256 with all filters 241 us then).  No row is sorted as a whole.
+//
+// The short way.  Every thread knows the largest of the values it loaded, one for each place of its four-value loads; the K-th
+// largest of these maxima has at least K values of the row at or above it, and seldom many more.  What lies above that bound (K = top_k, or 512 where top-p alone asks)
+// is sent to the first block, which sorts it and finishes alone, if the kept set turns out to lie inside.
+//
+// The long way, for flat rows, ties and large top_k.  The border of a filter is found by narrowing: the row's values between
+// two bounds are dropped into 16 buckets (equal steps of the float's ordered bit pattern, the last one open below), the blocks
+// add up their counts and masses, and the bucket that holds the border is the next range, until what lies above the range and
+// in it, or at least the range itself, is a list that one block can sort, or a single value.  Where the kept set is larger than a
+// list, a pass in the order of ids sums what is kept, 256 ids at a time.
 //
 // Masses are 64-bit sums of 64-bit exponentials: which id a number falls on hangs on the last bits of sums over the
-// vocabulary; with 128256 tokens fp32 would move the border of one row in a few hundred.  The exponential is table-driven (a
-// 64-entry table of powers of two and a polynomial of degree 5 on a 128th of an octave either side; the method of P. T. P.
-// Tang, ACM TOMS 15 (1989)), relative error below 1e-14.
+// vocabulary; with 128256 tokens fp32 would move the border of one row in a few hundred.  The exponential is table-driven (16
+// powers of two and a polynomial of degree 6 on a 32nd of an octave either side; the method of P. T. P. Tang, ACM TOMS 15
+// (1989)), relative error below 1e-14.  16 doubles are one row of the shared-memory banks: lookups do not conflict (64 entries
+// cost six cycles a warp, as much as the arithmetic).
 //
 // What bounds it: one row, the cluster barriers (a microsecond each); many rows, the 64-bit pipe where all of a row's
-// exponentials are needed (top-p alone, no filter at all), else the passes over shared memory.
+// exponentials are needed (top-p alone, no filter at all), else the passes over L2.
 #pragma once
 
 #include <type_traits>
@@ -27,15 +34,17 @@
 
 namespace dbt {
 
-constexpr int kSmThreads = 256;
-constexpr int kSmWarps = kSmThreads / 32;
-constexpr int kSmBuckets = 16;
+constexpr int kSmBuckets = 16;   // of a round by count; by mass kSmMassBuckets
+constexpr int kSmMassBuckets = 8;
 constexpr int kSmList = 1024;    // values that one block sorts
+constexpr int kSmGuess = 512;    // values that the short way asks for where top-k does not say, and its largest top_k
+constexpr int kSmMaxBuckets = 64;  // for the threads' maxima
+constexpr int kSmRun = 256;      // ids summed together by a warp on the long way
 constexpr int kSmMaxCluster = 8;
 constexpr int kSmMaxSlice = 32768;  // values of a row per block
-constexpr int kSmScratchBytes = kSmBuckets * kSmThreads * 8;  // bucket masses per thread, or the list's keys, w and sums
-static_assert(3 * kSmList * 8 <= kSmScratchBytes, "the list fits the scratch area");
-static_assert(kSmMaxSlice / kSmThreads <= 255, "counts of a thread fit a byte per bucket");
+// Scratch area: the list's keys, w and sums, or bucket masses per thread.
+constexpr int sm_scratch_bytes(int threads) { return 8 * (3 * kSmList > kSmMassBuckets * threads ? 3 * kSmList : kSmMassBuckets * threads); }
+static_assert(kSmMaxSlice / 256 <= 255, "counts of a thread fit a byte per bucket");
 
 struct SampleParams {
     const void *logits;
@@ -59,35 +68,92 @@ constexpr uint32_t kSmKeyLowest = 0x007fffffu;  // of -inf
 struct SampleShared {
     double exchange[2][kSmMaxCluster][2 * kSmBuckets];
     double local[2 * kSmBuckets];
-    double table[64];  // 2^(j / 64)
-    double warp_d[kSmWarps];
-    int warp_i[kSmWarps];
+    double table[16];  // 2^(j / 16)
+    double warp_d[32];
+    int warp_i[32];
     int counts[kSmBuckets];
-    int found;
+    int found, sent;
+    union {
+        struct {
+            int local[kSmMaxBuckets], all[kSmMaxCluster][kSmMaxBuckets];  // short way: the threads' maxima by bucket
+        } maxima;
+        struct {
+            double sums[kSmMaxSlice / kSmRun];  // long way: kept mass and ties of the border, per run of ids
+            int ties[kSmMaxSlice / kSmRun];
+        } runs;
+    };
 };
 
+template <typename T, int NT>
 struct SampleRow {
+    static constexpr int kWarps = NT / 32;
     SampleShared *sh;
-    float *x;        // this block's values
+    const T *src;  // this block's values
     double *scratch;
     int n, base;  // values held, id of the first
     uint32_t rank, cluster;
     int parity;
-    double top, step;  // largest value; 64 / (T ln 2)
-    bool top_inf;
+    double top, step;  // largest value; 16 / (T ln 2)
+    float zmin;        // smaller values weigh nothing: below 2^-1000, or (where the largest is infinite) not infinite
 
+    __device__ __forceinline__ void set_scale(float mx, float temp) {
+        const bool inf = mx == INFINITY;
+        top = inf ? 3.402823466e38 : mx;
+        step = inf ? 0.0 : 23.083120654223414 / (double)temp;  // 16 / ln 2
+        zmin = inf ? INFINITY : fmaxf(__double2float_ru(top - 16000.0 / step), -3.402823466e38f);
+    }
+    // Without a branch, so that several values' chains overlap.
     __device__ __forceinline__ double weight(float z) const {
-        if (top_inf) return z == INFINITY ? 1.0 : 0.0;
-        const double t = ((double)z - top) * step;  // exponent in 64ths of an octave
-        if (!(t > -64000.0) || z == -INFINITY) return 0.0;  // below 2^-1000
+        const double t = ((double)fminf(fmaxf(z, zmin), 3.402823466e38f) - top) * step;  // exponent in 16ths of an octave
         const double shifted = t + 6755399441055744.0;  // 1.5 * 2^52: rounds to an integer in the low bits
         const int i = __double2loint(shifted);
         const double r = t - (shifted - 6755399441055744.0);
-        // e^(r ln2 / 64) = 1 + r c + (r c)^2 / 2 + ..., |r c| <= 0.00542
-        constexpr double c = 0.010830424696249145;  // ln 2 / 64
-        const double p = fma(fma(fma(fma(fma(c * c * c * c * c / 120.0, r, c * c * c * c / 24.0), r, c * c * c / 6.0), r, c * c / 2.0), r, c), r, 1.0);
-        const double w = p * sh->table[i & 63];
-        return __hiloint2double(__double2hiint(w) + (i >> 6) * (1 << 20), __double2loint(w));
+        // e^(r ln2 / 16) = 1 + r c + (r c)^2 / 2 + ..., |r c| <= 0.0217
+        constexpr double c = 0.04332169878499658, c2 = c * c / 2.0, c3 = c2 * c / 3.0, c4 = c3 * c / 4.0, c5 = c4 * c / 5.0, c6 = c5 * c / 6.0;
+        const double p = fma(fma(fma(fma(fma(fma(c6, r, c5), r, c4), r, c3), r, c2), r, c), r, 1.0);
+        const double w = p * sh->table[i & 15];
+        const int hi = __double2hiint(w) + (i >> 4) * (1 << 20);
+        const bool any = z >= zmin;
+        return __hiloint2double(any ? hi : 0, any ? __double2loint(w) : 0);
+    }
+
+    static __device__ __forceinline__ float clean(float v) { return v != v ? -INFINITY : v + 0.f; }  // NaN counts as -inf; -0 becomes +0
+    __device__ __forceinline__ float at(int i) const { return clean(load1(src + i)); }
+    // f(i, z, m) for this thread's share of the block's values, m neighbours z[0..m) from number i on: fours out of 16-byte vectors,
+    // several in flight, and the single values before the first whole vector and after the last.
+    template <typename F>
+    __device__ __forceinline__ void each(F f) const {
+        constexpr int VN = 16 / sizeof(T), A = sizeof(T) == 4 ? 8 : 4;
+        const int tid = threadIdx.x, lead = min(n, (int)((16 - (reinterpret_cast<uintptr_t>(src) & 15)) & 15) / (int)sizeof(T));
+        const int vecs = (n - lead) / VN, tail = lead + vecs * VN;
+        const uint4 *v = reinterpret_cast<const uint4 *>(src + lead);
+        for (int i0 = tid; i0 < vecs; i0 += A * NT) {
+            uint4 raw[A];
+#pragma unroll
+            for (int a = 0; a < A; a++)
+                if (i0 + a * NT < vecs) raw[a] = __ldg(v + i0 + a * NT);
+#pragma unroll
+            for (int a = 0; a < A; a++) {
+                if (i0 + a * NT >= vecs) break;
+                const T *e = reinterpret_cast<const T *>(&raw[a]);
+#pragma unroll
+                for (int k = 0; k < VN; k += 4) {
+                    const float z[4] = {clean(load1(e + k)), clean(load1(e + k + 1)), clean(load1(e + k + 2)), clean(load1(e + k + 3))};
+                    f(lead + (i0 + a * NT) * VN + k, z, 4);
+                }
+            }
+        }
+        for (int s = 0; s < 2; s++) {
+            const int i = s == 0 ? tid : tail + tid;
+            if (i < (s == 0 ? lead : n)) {
+                const float z[4] = {at(i), 0.f, 0.f, 0.f};
+                f(i, z, 1);
+            }
+        }
+    }
+    // A list entry: pattern falling, id rising.
+    __device__ __forceinline__ void send(uint32_t addr, uint32_t k, int i) const {
+        asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(addr), "l"(((unsigned long long)~k << 32) | (uint32_t)(base + i)) : "memory");
     }
 
     // sh->local[0..nv) of every block becomes visible to all: returns the buffer [rank][2 * kSmBuckets].
@@ -96,10 +162,10 @@ struct SampleRow {
         double(*buf)[2 * kSmBuckets] = sh->exchange[parity];
         parity ^= 1;
         if (cluster == 1) {
-            for (int i = threadIdx.x; i < nv; i += kSmThreads) buf[0][i] = sh->local[i];
+            for (int i = threadIdx.x; i < nv; i += NT) buf[0][i] = sh->local[i];
             __syncthreads();
         } else {
-            for (int i = threadIdx.x; i < nv * (int)cluster; i += kSmThreads) {
+            for (int i = threadIdx.x; i < nv * (int)cluster; i += NT) {
                 const int to = i / nv, v = i - to * nv;
                 asm volatile("st.shared::cluster.f64 [%0], %1;" ::"r"(mapa_u32(smem_u32(&buf[rank][v]), to)), "d"(sh->local[v]) : "memory");
             }
@@ -115,7 +181,7 @@ struct SampleRow {
         __syncthreads();
         double t = 0.0;
 #pragma unroll
-        for (int w = 0; w < kSmWarps; w++) t += sh->warp_d[w];
+        for (int w = 0; w < NT / 32; w++) t += sh->warp_d[w];
         return t;
     }
     __device__ __forceinline__ int block_sum_i(int v) {
@@ -125,7 +191,7 @@ struct SampleRow {
         __syncthreads();
         int t = 0;
 #pragma unroll
-        for (int w = 0; w < kSmWarps; w++) t += sh->warp_i[w];
+        for (int w = 0; w < NT / 32; w++) t += sh->warp_i[w];
         return t;
     }
     // Sum over the cluster, in the order of the ranks.
@@ -139,10 +205,11 @@ struct SampleRow {
     }
 };
 
-// A border in falling order: values above tau are in, of those equal to it the first `ties` by id.
+// A border in falling order: values above tau are in, of those equal to it the first `ties` by id (all of them: `whole`).
 struct SampleBorder {
     uint32_t tau;
     int ties;
+    bool whole;
 };
 // A range of ordered bit patterns, what lies above it, and what it holds.
 struct SampleRange {
@@ -158,58 +225,72 @@ __device__ __forceinline__ int sm_ties(double mass, double each, int n) {
     return need >= 1.0 ? (need < (double)n ? (int)need : n) : 1;  // (0 / 0: one)
 }
 
-// One round: 16 buckets of 2^shift patterns from r.hi down, the last one open to r.lo.  MASS: by mass (goal), else by count.
-// `limit`: an earlier border; values outside it do not count.  total (first round): gets the mass of the whole range times
-// `share_p` as the goal.  Returns true when the border itself is found.
-template <bool MASS>
-__device__ __forceinline__ bool sm_round(SampleRow &row, SampleRange &r, int shift, double &goal, bool first, double share_p,
+// One round: buckets of 2^shift patterns from r.hi down, the last one open to r.lo.  MASS: by mass (goal), else by count.  `limit`: an
+// earlier border; values outside it do not count.  find_goal: the goal is the mass of all that lies in the range and above times share_p
+// (else the open bucket's mass is not needed, and not formed).  Returns true when the border itself is found.
+template <bool MASS, typename T, int NT>
+__device__ __forceinline__ bool sm_round(SampleRow<T, NT> &row, SampleRange &r, int shift, double &goal, bool find_goal, double share_p,
                                          const SampleBorder *limit, SampleBorder &found) {
+    constexpr int NB = MASS ? kSmMassBuckets : kSmBuckets;
     SampleShared &sh = *row.sh;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     unsigned long long c0 = 0, c1 = 0;
     if (MASS)
 #pragma unroll
-        for (int b = 0; b < kSmBuckets; b++) row.scratch[b * kSmThreads + tid] = 0.0;
+        for (int b = 0; b < NB; b++) row.scratch[b * NT + tid] = 0.0;
     if (tid < kSmBuckets) sh.counts[tid] = 0;
     const uint32_t lo = limit ? max(r.lo, limit->tau + 1) : r.lo;  // the border's own ties are added below
-    for (int i = tid; i < row.n; i += kSmThreads) {
-        const float z = row.x[i];
-        const uint32_t k = sm_key(z);
-        if (k > r.hi || k < lo) continue;
-        const int b = min((int)((r.hi - k) >> shift), kSmBuckets - 1);
-        const unsigned long long one = 1ull << (8 * (b & 7));
-        if (b < 8) c0 += one;
-        else c1 += one;
-        if (MASS) row.scratch[b * kSmThreads + tid] += row.weight(z);
-    }
+    const bool open = MASS && !find_goal && ((r.hi - r.lo) >> shift) >= NB;  // the last bucket's mass is not needed
+    row.each([&](int, const float(&z)[4], int m) {
+        int b[4];  // bucket, -1: outside
+        bool any = false;
+#pragma unroll
+        for (int e = 0; e < 4; e++) {
+            const uint32_t k = sm_key(z[e]);
+            const bool in = e < m && k <= r.hi && k >= lo;
+            b[e] = in ? min((int)((r.hi - k) >> shift), NB - 1) : -1;
+            const unsigned long long one = in ? 1ull << (8 * (b[e] & 7)) : 0ull;
+            if (NB <= 8 || b[e] < 8) c0 += one;
+            else c1 += one;
+            any = any || (in && !(open && b[e] == NB - 1));
+        }
+        if (MASS && any) {
+            double w[4];  // side by side, then into the buckets one after the other
+#pragma unroll
+            for (int e = 0; e < 4; e++) w[e] = row.weight(z[e]);
+#pragma unroll
+            for (int e = 0; e < 4; e++)
+                if (b[e] >= 0) row.scratch[b[e] * NT + tid] += w[e];
+        }
+    });
     __syncthreads();
 #pragma unroll
-    for (int b = 0; b < kSmBuckets; b++) {
+    for (int b = 0; b < NB; b++) {
         const int c = (int)(((b < 8 ? c0 : c1) >> (8 * (b & 7))) & 255);
         const int s = __reduce_add_sync(0xffffffffu, c);
         if (lane == b && s) atomicAdd(&sh.counts[b], s);
     }
     if (MASS)
-        for (int b = warp; b < kSmBuckets; b += kSmWarps) {
+        for (int b = warp; b < NB; b += NT / 32) {
             double v = 0.0;
 #pragma unroll
-            for (int j = 0; j < kSmThreads / 32; j++) v += row.scratch[b * kSmThreads + j * 32 + lane];
+            for (int j = 0; j < NT / 32; j++) v += row.scratch[b * NT + j * 32 + lane];
 #pragma unroll
             for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
             if (lane == 0) sh.local[b] = v;
         }
     __syncthreads();
-    if (tid < kSmBuckets) sh.local[kSmBuckets + tid] = sh.counts[tid];
+    if (tid < NB) sh.local[kSmBuckets + tid] = sh.counts[tid];
     const auto buf = row.share(2 * kSmBuckets);
     // lane b: bucket b over the blocks, then the running sums
     double w = 0.0, cw;
     long long c = 0, cc;
-    if (lane < kSmBuckets) {
+    if (lane < NB) {
         for (uint32_t k = 0; k < row.cluster; k++) {
             if (MASS) w += buf[k][lane];
             c += (long long)buf[k][kSmBuckets + lane];
         }
-        if (limit && limit->tau <= r.hi && limit->tau >= r.lo && (int)min((r.hi - limit->tau) >> shift, (uint32_t)(kSmBuckets - 1)) == lane) {
+        if (limit && limit->tau <= r.hi && limit->tau >= r.lo && (int)min((r.hi - limit->tau) >> shift, (uint32_t)(NB - 1)) == lane) {
             c += limit->ties;
             if (MASS) w += limit->ties * row.weight(sm_value(limit->tau));
         }
@@ -217,7 +298,7 @@ __device__ __forceinline__ bool sm_round(SampleRow &row, SampleRange &r, int shi
     cw = w;
     cc = c;
 #pragma unroll
-    for (int o = 1; o < kSmBuckets; o <<= 1) {
+    for (int o = 1; o < NB; o <<= 1) {
         const double a = __shfl_up_sync(0xffffffffu, cw, o);
         const long long d = __shfl_up_sync(0xffffffffu, cc, o);
         if (lane >= o) {
@@ -225,11 +306,11 @@ __device__ __forceinline__ bool sm_round(SampleRow &row, SampleRange &r, int shi
             cc += d;
         }
     }
-    if (MASS && first) goal = share_p * (r.above_w + __shfl_sync(0xffffffffu, cw, kSmBuckets - 1));
+    if (MASS && find_goal) goal = share_p * (r.above_w + __shfl_sync(0xffffffffu, cw, NB - 1));
     const bool reached = MASS ? r.above_w + cw >= goal : (double)(r.above_n + cc) >= goal;
-    const unsigned at = __ballot_sync(0xffffffffu, lane < kSmBuckets && c > 0 && reached);
-    const unsigned held = __ballot_sync(0xffffffffu, lane < kSmBuckets && c > 0);
-    // (a goal that rounding puts above the total: the last bucket that holds anything; the range always holds something)
+    const unsigned at = __ballot_sync(0xffffffffu, lane < NB && c > 0 && reached);
+    const unsigned held = __ballot_sync(0xffffffffu, lane < NB && c > 0);
+    // (a goal that rounding puts above the total, or in the open bucket: the last that holds anything; the range always holds something)
     const int j = at ? __ffs(at) - 1 : held ? 31 - __clz(held) : 0;
     r.above_w += __shfl_sync(0xffffffffu, cw - w, j);
     r.above_n += __shfl_sync(0xffffffffu, cc - c, j);
@@ -237,27 +318,29 @@ __device__ __forceinline__ bool sm_round(SampleRow &row, SampleRange &r, int shi
     const double in = __shfl_sync(0xffffffffu, w, j);
     const uint32_t hi = r.hi;
     r.hi = hi - ((uint32_t)j << shift);
-    const uint32_t span = 1u << shift;  // (shift <= 28)
-    if (j < kSmBuckets - 1 && r.hi - r.lo >= span) r.lo = r.hi - span + 1;
+    const uint32_t span = 1u << shift;  // (shift <= 29)
+    if (j < NB - 1 && r.hi - r.lo >= span) r.lo = r.hi - span + 1;
     if (r.hi != r.lo) return false;
     found.tau = r.hi;
-    if (MASS) {
-        found.ties = sm_ties(goal - r.above_w, in / (double)r.n, (int)r.n);
-    } else {
-        found.ties = (int)(goal - (double)r.above_n);
-    }
+    if (MASS) found.ties = sm_ties(goal - r.above_w, in / (double)r.n, (int)r.n);
+    else found.ties = (int)(goal - (double)r.above_n);
+    found.whole = found.ties >= r.n && !(limit && limit->tau == r.hi && !limit->whole);
     return true;
 }
 
 // Every value from pattern `lo` to `hi` into the first block's scratch as (pattern falling, id rising) keys; returns how many.
-__device__ __forceinline__ int sm_gather(SampleRow &row, uint32_t lo, uint32_t hi) {
+template <typename T, int NT>
+__device__ __forceinline__ int sm_gather(SampleRow<T, NT> &row, uint32_t lo, uint32_t hi) {
     SampleShared &sh = *row.sh;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     int mine = 0;
-    for (int i = tid; i < row.n; i += kSmThreads) {
-        const uint32_t k = sm_key(row.x[i]);
-        mine += k >= lo && k <= hi;
-    }
+    row.each([&](int, const float(&z)[4], int m) {
+#pragma unroll
+        for (int e = 0; e < 4; e++) {
+            const uint32_t k = sm_key(z[e]);
+            mine += e < m && k >= lo && k <= hi;
+        }
+    });
     int run = mine;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -269,7 +352,7 @@ __device__ __forceinline__ int sm_gather(SampleRow &row, uint32_t lo, uint32_t h
     __syncthreads();
     int at = run - mine, total = 0;
 #pragma unroll
-    for (int w = 0; w < kSmWarps; w++) {
+    for (int w = 0; w < NT / 32; w++) {
         if (w < warp) at += sh.warp_i[w];
         total += sh.warp_i[w];
     }
@@ -281,46 +364,96 @@ __device__ __forceinline__ int sm_gather(SampleRow &row, uint32_t lo, uint32_t h
         all += (int)buf[r][0];
     }
     const uint32_t list = mapa_u32(smem_u32(row.scratch), 0);
-    for (int i = tid; i < row.n; i += kSmThreads) {
-        const uint32_t k = sm_key(row.x[i]);
-        if (k >= lo && k <= hi) {
-            if (at < kSmList)  // (the callers have counted)
-                asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(list + 8 * at), "l"(((unsigned long long)~k << 32) | (uint32_t)(row.base + i)) : "memory");
-            at++;
+    row.each([&](int i, const float(&z)[4], int m) {
+#pragma unroll
+        for (int e = 0; e < 4; e++) {
+            const uint32_t k = sm_key(z[e]);
+            if (e < m && k >= lo && k <= hi) {
+                if (at < kSmList) row.send(list + 8 * at, k, i + e);  // (the callers have counted)
+                at++;
+            }
         }
-    }
+    });
     if (row.cluster == 1) __syncthreads();
     else cluster_sync_all();
     return min(all, kSmList);
 }
 
-// Bitonic sort of n <= kSmList keys by one block, rising.
-__device__ __forceinline__ void sm_sort(unsigned long long *key, int n) {
-    int m = 1;
-    while (m < n) m <<= 1;
-    for (int i = n + threadIdx.x; i < m; i += kSmThreads) key[i] = ~0ull;
-    __syncthreads();
-    for (int k = 2; k <= m; k <<= 1)
-        for (int j = k >> 1; j > 0; j >>= 1) {
-            for (int t = threadIdx.x; t < m / 2; t += kSmThreads) {
-                const int a = 2 * t - (t & (j - 1)), b = a + j;
-                const unsigned long long x = key[a], y = key[b];
-                if ((x > y) == ((a & k) == 0)) {
-                    key[a] = y;
-                    key[b] = x;
-                }
-            }
-            __syncthreads();
-        }
-}
-// Running sums of v[0..n) by one block, in order; 4 values per thread.
-__device__ __forceinline__ void sm_running(SampleShared &sh, const double *v, double *out, int n) {
-    static_assert(kSmList == 4 * kSmThreads, "four values a thread");
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    double a[4], sum = 0.0;
+// Bitonic merges inside a warp of keys that stand four to a lane (number = first + 4 lane + place): steps from distance `from` down.
+__device__ __forceinline__ void sm_merge(unsigned long long (&x)[4], int first, int k, int from) {
+    const int i0 = first + 4 * (threadIdx.x & 31);
+    auto order = [](unsigned long long &a, unsigned long long &b, bool rising) {
+        const bool swap = (a > b) == rising;
+        const unsigned long long s = swap ? b : a, l = swap ? a : b;
+        a = s;
+        b = l;
+    };
+    for (int j = from; j >= 4; j >>= 1) {
+        const bool least = ((i0 & j) == 0) == ((i0 & k) == 0);
 #pragma unroll
-    for (int k = 0; k < 4; k++) {
-        a[k] = 4 * tid + k < n ? v[4 * tid + k] : 0.0;
+        for (int q = 0; q < 4; q++) {
+            const unsigned long long y = __shfl_xor_sync(0xffffffffu, x[q], j >> 2);
+            x[q] = (x[q] < y) == least ? x[q] : y;
+        }
+    }
+    if (k >= 4) {
+        const bool rising = (i0 & k) == 0;
+        order(x[0], x[2], rising);
+        order(x[1], x[3], rising);
+        order(x[0], x[1], rising);
+        order(x[2], x[3], rising);
+    } else {
+        order(x[0], x[1], true);
+        order(x[2], x[3], false);
+    }
+}
+__device__ __forceinline__ void sm_sort_warp(unsigned long long (&x)[4], int first) {
+#pragma unroll 1
+    for (int k = 2; k <= 128; k <<= 1) sm_merge(x, first, k, k >> 1);
+}
+// Sort of n <= kSmList keys by one block, rising: 128 keys to a warp in registers, larger distances through shared memory.
+__device__ __forceinline__ void sm_sort(unsigned long long *key, int n) {
+    int m = 128;
+    while (m < n) m <<= 1;
+    __syncthreads();
+    const int i0 = 4 * (int)threadIdx.x, first = i0 & ~127;
+    if (i0 < m) {
+        unsigned long long x[4];
+#pragma unroll
+        for (int q = 0; q < 4; q++) x[q] = i0 + q < n ? key[i0 + q] : ~0ull;
+        sm_sort_warp(x, first);
+#pragma unroll 1
+        for (int k = 256; k <= m; k <<= 1) {
+#pragma unroll 1
+            for (int j = k >> 1; j >= 128; j >>= 1) {
+#pragma unroll
+                for (int q = 0; q < 4; q++) key[i0 + q] = x[q];
+                asm volatile("bar.sync 1, %0;" ::"r"(m / 4) : "memory");
+                const bool least = ((i0 & j) == 0) == ((i0 & k) == 0);
+#pragma unroll
+                for (int q = 0; q < 4; q++) {
+                    const unsigned long long y = key[(i0 ^ j) + q];
+                    x[q] = (x[q] < y) == least ? x[q] : y;
+                }
+                asm volatile("bar.sync 1, %0;" ::"r"(m / 4) : "memory");
+            }
+            sm_merge(x, first, k, 64);
+        }
+#pragma unroll
+        for (int q = 0; q < 4; q++) key[i0 + q] = x[q];
+    }
+    __syncthreads();
+}
+// Running sums of v[0..n) by one block, in order.
+template <int NT>
+__device__ __forceinline__ void sm_running(SampleShared &sh, const double *v, double *out, int n) {
+    constexpr int E = kSmList / NT;
+    static_assert(E * NT == kSmList && NT <= 1024, "the list is shared out evenly");
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    double a[E], sum = 0.0;
+#pragma unroll
+    for (int k = 0; k < E; k++) {
+        a[k] = E * tid + k < n ? v[E * tid + k] : 0.0;
         sum += a[k];
     }
     double run = sum;
@@ -338,11 +471,23 @@ __device__ __forceinline__ void sm_running(SampleShared &sh, const double *v, do
     for (int w = 0; w < warp; w++) base += sh.warp_d[w];
     base += before;
 #pragma unroll
-    for (int k = 0; k < 4; k++) {
+    for (int k = 0; k < E; k++) {
         base += a[k];
-        if (4 * tid + k < n) out[4 * tid + k] = base;
+        if (E * tid + k < n) out[E * tid + k] = base;
     }
     __syncthreads();
+}
+// Running sums of a warp's values, four to a lane in order; returns the sum before the lane's first.
+__device__ __forceinline__ double sm_running_warp(const double (&a)[4]) {
+    const int lane = threadIdx.x & 31;
+    double run = (a[0] + a[1]) + (a[2] + a[3]);
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const double x = __shfl_up_sync(0xffffffffu, run, o);
+        if (lane >= o) run += x;
+    }
+    const double before = __shfl_up_sync(0xffffffffu, run, 1);
+    return lane == 0 ? 0.0 : before;
 }
 
 struct SampleFilters {
@@ -352,46 +497,126 @@ struct SampleFilters {
 };
 
 // The first block finishes alone from the n largest values (keys in scratch).  goal: mass that top-p asks for, where it is
-// known; the list holds every survivor of top-k otherwise, or the whole row.
-__device__ __forceinline__ void sm_finish_list(SampleRow &row, const SampleParams &p, int r, const SampleFilters &f, int n, bool goal_known,
-                                               double goal) {
+// known; the list holds every survivor of top-k otherwise, or the whole row.  guess: the list may be too short for what
+// top-p and min-p keep; false then, nothing is written, and *mass gets what the list weighs.
+template <typename T, int NT>
+__device__ __forceinline__ bool sm_finish_list(SampleRow<T, NT> &row, const SampleParams &p, int r, const SampleFilters &f, int n, bool goal_known,
+                                               double goal, bool guess, double *mass) {
     SampleShared &sh = *row.sh;
     const int tid = threadIdx.x;
     unsigned long long *key = reinterpret_cast<unsigned long long *>(row.scratch);
     double *w = row.scratch + kSmList, *run = row.scratch + 2 * kSmList;
+    if (n <= 128) {  // one warp, without barriers
+        __syncthreads();
+        if (tid < 32) {
+            const int i0 = 4 * tid;
+            unsigned long long x[4];
+#pragma unroll
+            for (int q = 0; q < 4; q++) x[q] = i0 + q < n ? key[i0 + q] : ~0ull;
+            sm_sort_warp(x, 0);
+            if (f.k_on) n = min(n, f.k);
+            double v[4];
+#pragma unroll
+            for (int q = 0; q < 4; q++) v[q] = i0 + q < n ? row.weight(sm_value(~(uint32_t)(x[q] >> 32))) : 0.0;
+            double upto = sm_running_warp(v);
+            const double whole = __shfl_sync(0xffffffffu, upto + ((v[0] + v[1]) + (v[2] + v[3])), 31);
+            if (f.p_on && !goal_known) goal = f.p * whole;
+            int in_p = 0, in_m = 0;
+#pragma unroll
+            for (int q = 0; q < 4; q++) {
+                upto += v[q];
+                in_p += i0 + q < n && upto < goal;
+                in_m += i0 + q < n && v[q] >= f.m;
+            }
+            in_p = f.p_on ? __reduce_add_sync(0xffffffffu, in_p) : n;
+            in_m = f.m_on ? __reduce_add_sync(0xffffffffu, in_m) : n;
+            const int keep = max(1, min(min(n, in_p + 1), in_m));
+            const bool inside = in_p < n || in_m < n;  // the kept set ends within the list
+            if (tid == 0) sh.found = !guess || inside;
+            if (guess && !inside) {
+                if (tid == 0) *mass = whole;
+            } else {
+                // the kept ones by id
+                __syncwarp();
+#pragma unroll
+                for (int q = 0; q < 4; q++) {
+                    w[i0 + q] = v[q];
+                    x[q] = i0 + q < keep ? (x[q] << 32) | (uint32_t)(i0 + q) : ~0ull;
+                }
+                sm_sort_warp(x, 0);
+                __syncwarp();
+#pragma unroll
+                for (int q = 0; q < 4; q++) v[q] = i0 + q < keep ? w[(uint32_t)x[q]] : 0.0;
+                double before = sm_running_warp(v);
+                const double total = __shfl_sync(0xffffffffu, before + ((v[0] + v[1]) + (v[2] + v[3])), 31), target = f.u * total;
+                int at = -1;  // the lane's first place past the target, or else its last with any weight
+                bool past = false;
+#pragma unroll
+                for (int q = 0; q < 4; q++) {
+                    before += v[q];
+                    if (v[q] > 0.0 && !past) {
+                        at = q;
+                        past = before > target;
+                    }
+                }
+                const unsigned hit = __ballot_sync(0xffffffffu, past), any = __ballot_sync(0xffffffffu, at >= 0);
+                if (tid == (hit ? __ffs(hit) - 1 : 31 - __clz(any))) {
+                    unsigned long long id = x[0];
+                    double mine = v[0];
+#pragma unroll
+                    for (int q = 1; q < 4; q++)
+                        if (q == at) {
+                            id = x[q];
+                            mine = v[q];
+                        }
+                    p.tokens[r] = (int32_t)(id >> 32);
+                    if (p.logprobs) p.logprobs[r] = (float)log(mine / total);
+                }
+            }
+        }
+        __syncthreads();
+        return sh.found != 0;
+    }
     sm_sort(key, n);
     if (f.k_on) n = min(n, f.k);
-    for (int i = tid; i < n; i += kSmThreads) w[i] = row.weight(sm_value(~(uint32_t)(key[i] >> 32)));
+    for (int i = tid; i < n; i += NT) w[i] = row.weight(sm_value(~(uint32_t)(key[i] >> 32)));
     __syncthreads();
     int keep = n;
     if (f.p_on || f.m_on) {
-        if (f.p_on) sm_running(sh, w, run, n);
+        if (f.p_on) sm_running<NT>(sh, w, run, n);
         if (f.p_on && !goal_known) goal = f.p * run[n - 1];
         int in_p = 0, in_m = 0;
-        for (int i = tid; i < n; i += kSmThreads) {
+        for (int i = tid; i < n; i += NT) {
             in_p += f.p_on && run[i] < goal;
             in_m += f.m_on && w[i] >= f.m;
         }
-        if (f.p_on) keep = min(keep, row.block_sum_i(in_p) + 1);
-        if (f.m_on) keep = min(keep, row.block_sum_i(in_m));
+        if (f.p_on) in_p = row.block_sum_i(in_p);
+        if (f.m_on) in_m = row.block_sum_i(in_m);
+        const bool inside = (f.p_on && in_p < n) || (f.m_on && in_m < n);  // the kept set ends within the list
+        if (guess && !inside) {
+            *mass = run[n - 1];
+            return false;
+        }
+        if (f.p_on) keep = min(keep, in_p + 1);
+        if (f.m_on) keep = min(keep, in_m);
         keep = max(keep, 1);
     }
     // the kept ones by id, their weights' places beside
-    for (int i = tid; i < keep; i += kSmThreads) {
+    for (int i = tid; i < keep; i += NT) {
         const unsigned long long k = key[i];
         key[i] = (k << 32) | (uint32_t)i;
     }
     __syncthreads();
     sm_sort(key, keep);
     double *wi = run;  // weights by id, then their running sums over the weights' old place
-    for (int i = tid; i < keep; i += kSmThreads) wi[i] = w[(uint32_t)key[i]];
+    for (int i = tid; i < keep; i += NT) wi[i] = w[(uint32_t)key[i]];
     __syncthreads();
-    sm_running(sh, wi, w, keep);
+    sm_running<NT>(sh, wi, w, keep);
     const double total = w[keep - 1], target = f.u * total;
     if (tid == 0) sh.found = kSmList;
     __syncthreads();
     int first = kSmList, last = -1;
-    for (int i = tid; i < keep; i += kSmThreads) {
+    for (int i = tid; i < keep; i += NT) {
         if (first == kSmList && w[i] > target) first = i;
         if (wi[i] > 0.0) last = i;
     }
@@ -410,16 +635,16 @@ __device__ __forceinline__ void sm_finish_list(SampleRow &row, const SampleParam
         p.tokens[r] = (int32_t)(key[at] >> 32);
         if (p.logprobs) p.logprobs[r] = (float)log(wi[at] / total);
     }
+    return true;
 }
 
-template <typename T>
-__global__ void __launch_bounds__(kSmThreads) sample_kernel(const SampleParams p) {
+template <typename T, int NT>
+__global__ void __launch_bounds__(NT, NT == 256 ? 4 : 1) sample_kernel(const SampleParams p) {
     extern __shared__ __align__(16) uint8_t smem_b[];
     __shared__ SampleShared sh;
-    SampleRow row;
+    SampleRow<T, NT> row;
     row.sh = &sh;
     row.scratch = reinterpret_cast<double *>(smem_b);
-    row.x = reinterpret_cast<float *>(smem_b + kSmScratchBytes);
     row.parity = 0;
     row.rank = cluster_rank();
     asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(row.cluster));
@@ -427,29 +652,16 @@ __global__ void __launch_bounds__(kSmThreads) sample_kernel(const SampleParams p
     const int r = blockIdx.x / row.cluster;
     row.base = row.rank * p.slice;
     row.n = max(0, min(p.slice, p.vocab - row.base));
+    row.src = reinterpret_cast<const T *>(p.logits) + (long long)r * p.row_stride + row.base;
 
-    // ---- the row into shared memory, its largest value
-    const T *src = reinterpret_cast<const T *>(p.logits) + (long long)r * p.row_stride + row.base;
-    float mx = -INFINITY;
-    auto put = [&](int i, float v) {
-        v = v != v ? -INFINITY : v + 0.f;  // NaN counts as -inf; -0 becomes +0
-        row.x[i] = v;
-        mx = fmaxf(mx, v);
-    };
-    constexpr int VN = 16 / sizeof(T);
-    int head = 0;
-    if ((reinterpret_cast<uintptr_t>(src) & 15) == 0) {
-        head = row.n / VN * VN;
-#pragma unroll 4
-        for (int i = tid * VN; i < head; i += kSmThreads * VN) {
-            const uint4 raw = __ldg(reinterpret_cast<const uint4 *>(src + i));
-            const T *e = reinterpret_cast<const T *>(&raw);
+    // ---- the row's largest value
+    float own[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};  // by place in the fours
+    row.each([&](int, const float(&z)[4], int m) {
 #pragma unroll
-            for (int k = 0; k < VN; k++) put(i + k, load1(e + k));
-        }
-    }
-    for (int i = head + tid; i < row.n; i += kSmThreads) put(i, load1(src + i));
-    if (tid < 64) sh.table[tid] = exp2(tid / 64.0);
+        for (int e = 0; e < 4; e++)
+            if (e < m) own[e] = fmaxf(own[e], z[e]);
+    });
+    if (tid < 16) sh.table[tid] = exp2(tid / 16.0);
     SampleFilters f;
     const float temp = p.temperature ? p.temperature[r] : 1.f;
     f.u = p.uniforms[r];
@@ -461,15 +673,26 @@ __global__ void __launch_bounds__(kSmThreads) sample_kernel(const SampleParams p
     f.k_on = f.k > 0 && f.k < p.vocab;
     f.p_on = !(f.p >= 1.0);
     if (f.p != f.p) f.p = 0.0;
-    mx = block_max(mx, reinterpret_cast<float *>(sh.warp_d));
-    if (tid == 0) sh.local[0] = mx;
-    {
-        const auto buf = row.share(1);
-        for (uint32_t k = 0; k < row.cluster; k++) mx = fmaxf(mx, (float)buf[k][0]);
+    const float own_max = fmaxf(fmaxf(own[0], own[1]), fmaxf(own[2], own[3]));
+    float mx = block_max(own_max, reinterpret_cast<float *>(sh.warp_d));
+    float low_max = INFINITY;  // the lowest of the maxima, without values that stand for -inf
+#pragma unroll
+    for (int e = 0; e < 4; e++) low_max = own[e] > -1e4f ? fminf(low_max, own[e]) : low_max;
+    low_max = -block_max(-low_max, reinterpret_cast<float *>(sh.warp_d));
+    if (tid == 0) {
+        sh.local[0] = mx;
+        sh.local[1] = low_max;
+        sh.sent = 0;
     }
-    row.top = mx;
-    row.top_inf = mx == INFINITY;
-    row.step = 92.332482616893657 / (double)temp;  // 64 / ln 2
+    if (tid < kSmMaxBuckets) sh.maxima.local[tid] = 0;
+    {
+        const auto buf = row.share(2);
+        for (uint32_t k = 0; k < row.cluster; k++) {
+            mx = fmaxf(mx, (float)buf[k][0]);
+            low_max = fminf(low_max, (float)buf[k][1]);
+        }
+    }
+    row.set_scale(mx, temp);
     if (mx == -INFINITY) {
         if (row.rank == 0 && tid == 0) {
             p.tokens[r] = -1;
@@ -479,12 +702,16 @@ __global__ void __launch_bounds__(kSmThreads) sample_kernel(const SampleParams p
     }
     if (!(temp > 0.f)) {  // the largest logit, the lowest id of several
         int best = 0x7fffffff;
-        for (int i = tid; i < row.n; i += kSmThreads)
-            if (row.x[i] == mx) best = min(best, row.base + i);
+        if (own_max == mx)  // (few threads)
+            row.each([&](int i, const float(&z)[4], int m) {
+#pragma unroll
+                for (int e = 0; e < 4; e++)
+                    if (e < m && z[e] == mx) best = min(best, row.base + i + e);
+            });
         best = __reduce_min_sync(0xffffffffu, best);
         if (lane == 0) sh.warp_i[warp] = best;
         __syncthreads();
-        for (int w = 0; w < kSmWarps; w++) best = min(best, sh.warp_i[w]);
+        for (int w = 0; w < NT / 32; w++) best = min(best, sh.warp_i[w]);
         if (tid == 0) sh.local[0] = best;
         const auto buf = row.share(1);
         for (uint32_t k = 0; k < row.cluster; k++) best = min(best, (int)buf[k][0]);
@@ -495,27 +722,141 @@ __global__ void __launch_bounds__(kSmThreads) sample_kernel(const SampleParams p
         return;
     }
 
-    // ---- the borders
     const uint32_t key_top = sm_key(mx);
-    SampleBorder border{0, 0};  // everything
+    struct {
+        bool on;
+        double total;
+        SampleRange range;
+    } known{};
+    // ---- the short way
+    const int most = min(kSmGuess, 2 * NT * (int)row.cluster);  // (at most half of the maxima: the bound stays high)
+    if (p.vocab > kSmList && (f.k_on ? f.k <= most : f.p_on || f.m_on)) {
+        uint32_t lo = key_top;
+        bool bound = false;
+        if (!f.k_on && !f.p_on) {
+            // w >= m is z >= max + T ln m; a little below that, whatever the roundings: the list's own test is the exact one
+            const double low = row.top + (double)temp * (log(f.m) - 1e-6);
+            if (mx < INFINITY) lo = max(kSmKeyLowest, sm_key(__double2float_rd(low) + 0.f));
+            bound = true;
+        } else {
+            // equal steps from the largest value down to the lowest of the maxima
+            const float per = kSmMaxBuckets / (low_max < mx ? mx - low_max : 32.f);
+#pragma unroll
+            for (int e = 0; e < 4; e++) atomicAdd(&sh.maxima.local[(int)fminf((mx - own[e]) * per, (float)(kSmMaxBuckets - 1))], 1);
+            __syncthreads();
+            for (int i = tid; i < kSmMaxBuckets * (int)row.cluster; i += NT) {
+                const int to = i / kSmMaxBuckets, b = i - to * kSmMaxBuckets;
+                asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(mapa_u32(smem_u32(&sh.maxima.all[row.rank][b]), to)), "r"(sh.maxima.local[b]) : "memory");
+            }
+            if (row.cluster == 1) __syncthreads();
+            else cluster_sync_all();
+            int a = 0, b = 0;  // buckets 2 lane, 2 lane + 1
+            for (uint32_t k = 0; k < row.cluster; k++) {
+                a += sh.maxima.all[k][2 * lane];
+                b += sh.maxima.all[k][2 * lane + 1];
+            }
+            int run = a + b;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const int v = __shfl_up_sync(0xffffffffu, run, o);
+                if (lane >= o) run += v;
+            }
+            const int want = f.k_on ? f.k : most;
+            const unsigned at = __ballot_sync(0xffffffffu, run >= want);
+            const int l = at ? __ffs(at) - 1 : 31, before = __shfl_sync(0xffffffffu, run - a - b, l), first = __shfl_sync(0xffffffffu, a, l);
+            const int j = 2 * l + (before + first < want);
+            // the bucket's lower end, and a little below that for the roundings; the last bucket is open: no bound
+            bound = at && j < kSmMaxBuckets - 1 && mx < INFINITY;
+            if (bound) lo = sm_key(mx - (j + 1.01f) / per + 0.f);
+        }
+        if (bound) {
+            // what lies at or above it to the first block, a part of the list's second place for each; with top-p alone also the total
+            const int part = kSmList / (int)row.cluster;
+            const uint32_t list = mapa_u32(smem_u32(row.scratch + kSmList + row.rank * part), 0);
+            const bool all = f.p_on && !f.k_on;
+            double total = 0.0;
+            const float lo_value = sm_value(lo);  // (the cleaned values are in the order of their patterns)
+            auto pick = [&](int i, const float(&z)[4], int m) {
+                if (m == 4 ? fmaxf(fmaxf(z[0], z[1]), fmaxf(z[2], z[3])) < lo_value : z[0] < lo_value) return;
+#pragma unroll
+                for (int e = 0; e < 4; e++)
+                    if (e < m && z[e] >= lo_value) {
+                        const int at = atomicAdd(&sh.sent, 1);
+                        if (at < part) row.send(list + 8 * at, sm_key(z[e]), i + e);
+                    }
+            };
+            if (all)
+                row.each([&](int i, const float(&z)[4], int m) {
+                    total += m == 4 ? (row.weight(z[0]) + row.weight(z[1])) + (row.weight(z[2]) + row.weight(z[3])) : row.weight(z[0]);
+                    pick(i, z, m);
+                });
+            else
+                row.each(pick);
+            if (all) total = row.block_sum_d(total);
+            __syncthreads();
+            if (tid == 0) {
+                sh.local[0] = sh.sent;
+                sh.local[1] = total;
+            }
+            const auto buf = row.share(2);
+            bool fits = true;
+            total = 0.0;
+            int n = 0, from[kSmMaxCluster + 1];
+#pragma unroll
+            for (int k = 0; k < kSmMaxCluster; k++) {
+                from[k] = n;
+                if (k < (int)row.cluster) {
+                    n += (int)buf[k][0];
+                    total += buf[k][1];
+                    fits = fits && buf[k][0] <= part;
+                }
+            }
+            from[kSmMaxCluster] = n;
+            if (fits && (!f.k_on || n >= f.k)) {  // (n < k: roundings wider than the buckets)
+                bool done = true;
+                double mass = 0.0;
+                if (row.rank == 0) {
+                    unsigned long long *key = reinterpret_cast<unsigned long long *>(row.scratch), *raw = key + kSmList;
+#pragma unroll
+                    for (int k = 0; k < kSmMaxCluster; k++)
+                        for (int i = tid; i < from[k + 1] - from[k]; i += NT) key[from[k] + i] = raw[k * part + i];
+                    __syncthreads();
+                    done = sm_finish_list(row, p, r, f, n, all, f.p * total, all, &mass);
+                }
+                if (!all) return;  // (the list holds all that top-k, or min-p, keeps)
+                if (tid == 0) {
+                    sh.local[0] = done;
+                    sh.local[1] = mass;
+                }
+                const auto verdict = row.share(2);
+                if (verdict[0][0] != 0.0) return;
+                // top-p reaches further down: the long way begins below the list
+                known.total = total;
+                known.range = SampleRange{kSmKeyLowest, lo - 1, n, verdict[0][1], 0};
+                known.on = lo > kSmKeyLowest;
+            }
+        }
+    }
+
+    // ---- the long way: the borders
+    SampleBorder border{0, 0, true};  // everything
     bool bounded = false;
-    auto narrow = [&](auto mass, double &goal, const SampleBorder *limit, SampleRange &range, SampleBorder &found) -> int {
+    auto narrow = [&](auto mass, double &goal, bool find_goal, const SampleBorder *limit, SampleRange &range, SampleBorder &found) -> int {
         // 1: the values from range.lo up fit the list; 2: `found` is the border
         constexpr bool MASS = decltype(mass)::value;
+        constexpr int NB = MASS ? kSmMassBuckets : kSmBuckets, BITS = MASS ? 3 : 4;
         // The first window reaches 8 units below the largest value (counts), 8 T (masses): about where the border lies in a
         // language model's logits.  A border below it is looked for in a window 16 times as wide, then in all that is left.
         float reach = MASS ? 8.f * temp : 8.f;
-        range = SampleRange{kSmKeyLowest, key_top, 0, 0.0, 0};
-        for (int it = 0; it < 16; it++) {  // (two rounds of windows, then eight at most: a round takes four of 32 bits)
-            const uint32_t full = range.hi - range.lo;
-            uint32_t span = full;
+        for (int it = 0; it < 16; it++) {  // (two rounds of windows, then eleven at most: a round takes three of 32 bits, or four)
+            uint32_t span = range.hi - range.lo;
             if (range.lo == kSmKeyLowest && it < 2) {
                 const uint32_t low = sm_key(sm_value(range.hi) - reach);  // (not a number: above, the full range)
                 if (low < range.hi && low > range.lo) span = range.hi - low;
                 reach *= 16.f;
             }
-            const int shift = 28 - __clz(span | 15);  // 16 buckets cover span + 1 patterns
-            const bool exact = sm_round<MASS>(row, range, shift, goal, it == 0, f.p, limit, found);
+            const int shift = 32 - BITS - __clz(span | (NB - 1));  // the buckets cover span + 1 patterns
+            const bool exact = sm_round<MASS>(row, range, shift, goal, find_goal && it == 0, f.p, limit, found);
             if (exact) return 2;
             if (!limit && range.above_n + range.n <= kSmList) return 1;
             if (range.n <= kSmList) {
@@ -529,38 +870,44 @@ __global__ void __launch_bounds__(kSmThreads) sample_kernel(const SampleParams p
                     sm_sort(key, n);
                     int at;  // number of values of the range above the border
                     if (MASS) {
-                        for (int i = tid; i < n; i += kSmThreads) w[i] = row.weight(sm_value(~(uint32_t)(key[i] >> 32)));
+                        for (int i = tid; i < n; i += NT) w[i] = row.weight(sm_value(~(uint32_t)(key[i] >> 32)));
                         __syncthreads();
-                        sm_running(sh, w, run, n);
+                        sm_running<NT>(sh, w, run, n);
                         int before = 0;
-                        for (int i = tid; i < n; i += kSmThreads) before += range.above_w + run[i] < goal;
+                        for (int i = tid; i < n; i += NT) before += range.above_w + run[i] < goal;
                         at = row.block_sum_i(before);
                         if (!ends) at = min(at, n - 1);
                     } else {
                         at = (int)(goal - (double)range.above_n) - 1;
                     }
                     uint32_t tau;
-                    int same = 0;
+                    int same = 0, more = 0;  // ties up to the border, and beyond it
                     if (at < n) {
                         tau = ~(uint32_t)(key[at] >> 32);
-                        for (int i = tid; i <= at; i += kSmThreads) same += (uint32_t)(key[i] >> 32) == ~tau;
+                        for (int i = tid; i < n; i += NT) {
+                            const bool tie = (uint32_t)(key[i] >> 32) == ~tau;
+                            same += tie && i <= at;
+                            more += tie && i > at;
+                        }
                         same = row.block_sum_i(same);
+                        more = row.block_sum_i(more);
                     } else {
                         tau = limit->tau;
                         same = sm_ties(goal - range.above_w - (n > 0 ? run[n - 1] : 0.0), row.weight(sm_value(tau)), limit->ties);
+                        more = same < limit->ties || !limit->whole;
                     }
                     if (tid == 0) {
                         sh.local[0] = tau;
                         sh.local[1] = same;
+                        sh.local[2] = more;
                     }
                 }
-                const auto buf = row.share(2);
-                found.tau = (uint32_t)buf[0][0];
-                found.ties = (int)buf[0][1];
+                const auto buf = row.share(3);
+                found = SampleBorder{(uint32_t)buf[0][0], (int)buf[0][1], buf[0][2] == 0.0};
                 return 2;
             }
         }
-        found = SampleBorder{range.hi, 1};
+        found = SampleBorder{range.hi, 1, false};
         return 2;
     };
 
@@ -569,12 +916,14 @@ __global__ void __launch_bounds__(kSmThreads) sample_kernel(const SampleParams p
     double goal = 0.0;
     if (!listed && f.k_on) {
         goal = f.k;
-        if (narrow(std::false_type{}, goal, nullptr, range, border) == 1) listed = true;
+        if (narrow(std::false_type{}, goal, false, nullptr, range, border) == 1) listed = true;
         else bounded = true;
     }
     if (!listed && f.p_on) {
         SampleBorder other;
-        const int how = narrow(std::true_type{}, goal, bounded ? &border : nullptr, range, other);
+        range = known.on ? known.range : SampleRange{kSmKeyLowest, key_top, 0, 0.0, p.vocab};
+        goal = f.p * known.total;
+        const int how = narrow(std::true_type{}, goal, !known.on, bounded ? &border : nullptr, range, other);
         goal_known = true;
         if (how == 1) {
             listed = true;
@@ -583,119 +932,162 @@ __global__ void __launch_bounds__(kSmThreads) sample_kernel(const SampleParams p
             border = other;  // (never below top-k's: masses were counted inside it)
             bounded = true;
         }
-    } else if (!listed && !bounded && f.m_on) {
-        // w >= m is z >= max + T ln m; a little below that, whatever the roundings: the list's own test is the exact one
-        const double low = row.top + (double)temp * (log(f.m) - 1e-6);
-        const uint32_t lo = row.top_inf ? key_top : max(kSmKeyLowest, sm_key(__double2float_rd(low) + 0.f));
-        int c = 0;
-        for (int i = tid; i < row.n; i += kSmThreads) c += sm_key(row.x[i]) >= lo;
-        if (row.sum_all((double)c) <= kSmList) {
-            listed = true;
-            range.lo = lo;
-        }
     }
     if (listed) {
         const int n = sm_gather(row, range.lo, key_top);
-        if (row.rank == 0) sm_finish_list(row, p, r, f, n, goal_known, goal);
+        if (row.rank == 0) sm_finish_list(row, p, r, f, n, goal_known, goal, false, nullptr);
         return;
     }
 
-    // ---- many values are kept: sums in the order of ids.  Warp w of a block has a run of consecutive values.
-    const int per = ((p.slice + kSmWarps - 1) / kSmWarps + 31) & ~31, i0 = min(row.n, warp * per), i1 = min(row.n, i0 + per);
-    int ties_before = 0;
-    if (bounded) {
-        int c = 0;
-        for (int i = i0 + lane; i < i1; i += 32) c += sm_key(row.x[i]) == border.tau;
-        c = __reduce_add_sync(0xffffffffu, c);
-        __syncthreads();
-        if (lane == 0) sh.warp_i[warp] = c;
-        __syncthreads();
-        int all = 0;
-        for (int w = 0; w < kSmWarps; w++) {
-            if (w < warp) ties_before += sh.warp_i[w];
-            all += sh.warp_i[w];
+    // ---- many values are kept: sums in the order of ids, a warp per run of kSmRun of them, eight neighbours a lane
+    const int runs = (row.n + kSmRun - 1) / kSmRun;
+    const bool ranked = bounded && !border.whole;  // some of the border's ties stay out: their order counts
+    const bool vectors = (reinterpret_cast<uintptr_t>(row.src) & 15) == 0;
+    auto values = [&](int q, float(&z)[8]) {
+        const int i = q * kSmRun + lane * 8;
+        if (vectors && i + 8 <= row.n) {
+            load8(row.src + i, z);
+#pragma unroll
+            for (int e = 0; e < 8; e++) z[e] = row.clean(z[e]);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; e++) z[e] = i + e < row.n ? row.at(i + e) : -INFINITY;  // (behind the last: no weight)
         }
-        if (tid == 0) sh.local[0] = all;
+    };
+    auto count_ties = [&](const float(&z)[8], int q) {
+        int c = 0;
+#pragma unroll
+        for (int e = 0; e < 8; e++) c += sm_key(z[e]) == border.tau && q * kSmRun + lane * 8 + e < row.n;
+        return c;
+    };
+    // the kept weights of a lane's eight values; `seen`: the border's ties before run q
+    auto weigh = [&](int q, int seen, double(&w)[8]) {
+        float z[8];
+        values(q, z);
+#pragma unroll
+        for (int e = 0; e < 8; e++) w[e] = row.weight(z[e]);
+        if (!bounded && !f.m_on) return;
+        if (ranked) {
+            const int mine = count_ties(z, q);
+            int run = mine;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const int v = __shfl_up_sync(0xffffffffu, run, o);
+                if (lane >= o) run += v;
+            }
+            seen += run - mine;
+        }
+#pragma unroll
+        for (int e = 0; e < 8; e++) {
+            const uint32_t k = sm_key(z[e]);
+            bool in = !bounded || k > border.tau;
+            if (bounded && k == border.tau) in = border.whole || seen++ < border.ties;
+            if (!in || (f.m_on && w[e] < f.m)) w[e] = 0.0;
+        }
+    };
+    __syncthreads();
+    int ties_before = 0;  // of the blocks before
+    if (ranked) {
+        for (int q = warp; q < runs; q += NT / 32) {
+            float z[8];
+            values(q, z);
+            const int c = __reduce_add_sync(0xffffffffu, count_ties(z, q));
+            if (lane == 0) sh.runs.ties[q] = c;
+        }
+        __syncthreads();
+        if (warp == 0) {  // running sums, each without its own
+            int base = 0;
+            for (int q0 = 0; q0 < runs; q0 += 32) {
+                const int mine = q0 + lane < runs ? sh.runs.ties[q0 + lane] : 0;
+                int run = mine;
+#pragma unroll
+                for (int o = 1; o < 32; o <<= 1) {
+                    const int v = __shfl_up_sync(0xffffffffu, run, o);
+                    if (lane >= o) run += v;
+                }
+                if (q0 + lane < runs) sh.runs.ties[q0 + lane] = base + run - mine;
+                base += __shfl_sync(0xffffffffu, run, 31);
+            }
+            if (lane == 0) sh.local[0] = base;
+        }
         const auto buf = row.share(1);
         for (uint32_t k = 0; k < row.rank; k++) ties_before += (int)buf[k][0];
     }
-    // the weight of value i, zero where it is not kept; `seen` counts the border's ties before the warp's 32
-    auto kept = [&](int i, int &seen) -> double {
-        const float z = i < i1 ? row.x[i] : 0.f;
-        const uint32_t k = sm_key(z);
-        bool in = i < i1 && (!bounded || k > border.tau);
-        if (bounded) {
-            const bool tie = i < i1 && k == border.tau;
-            const unsigned m = __ballot_sync(0xffffffffu, tie);
-            in = in || (tie && seen + __popc(m & ((1u << lane) - 1)) < border.ties);
-            seen += __popc(m);
-        }
-        if (!in) return 0.0;
-        const double w = row.weight(z);
-        return f.m_on && w < f.m ? 0.0 : w;
-    };
-    double mine = 0.0;
-    int seen = ties_before;
-    for (int i = i0 + lane; i - lane < i1; i += 32) mine += kept(i, seen);
+    for (int q = warp; q < runs; q += NT / 32) {
+        double w[8];
+        weigh(q, ranked ? ties_before + sh.runs.ties[q] : 0, w);
+        double mine = ((w[0] + w[1]) + (w[2] + w[3])) + ((w[4] + w[5]) + (w[6] + w[7]));
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) mine += __shfl_xor_sync(0xffffffffu, mine, o);
+        for (int o = 16; o > 0; o >>= 1) mine += __shfl_xor_sync(0xffffffffu, mine, o);
+        if (lane == 0) sh.runs.sums[q] = mine;
+    }
     __syncthreads();
-    if (lane == 0) sh.warp_d[warp] = mine;
-    __syncthreads();
-    double all = 0.0, total = 0.0;
-    for (int w = 0; w < kSmWarps; w++) all += sh.warp_d[w];
-    if (tid == 0) sh.local[0] = all;
+    if (warp == 0) {  // running sums of the runs
+        double base = 0.0;
+        for (int q0 = 0; q0 < runs; q0 += 32) {
+            double run = q0 + lane < runs ? sh.runs.sums[q0 + lane] : 0.0;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const double v = __shfl_up_sync(0xffffffffu, run, o);
+                if (lane >= o) run += v;
+            }
+            if (q0 + lane < runs) sh.runs.sums[q0 + lane] = base + run;
+            base += __shfl_sync(0xffffffffu, run, 31);
+        }
+        if (lane == 0) sh.local[0] = base;
+    }
     const auto sums = row.share(1);
-    double base = 0.0, run = 0.0;
+    double total = 0.0, base = 0.0, upto = 0.0;
     for (uint32_t k = 0; k < row.cluster; k++) total += sums[k][0];
     const double target = f.u * total;
-    // the block, then the warp in whose run the target lies; the last with any mass takes what rounding leaves over
+    // the block, then the run that the target lies in; the last with any mass takes what rounding leaves over
     int owner = -1, last = 0;
     for (uint32_t k = 0; k < row.cluster && owner < 0; k++) {
-        if (k == row.rank) base = run;
-        run += sums[k][0];
-        if (sums[k][0] > 0.0) last = k;
-        if (run > target) owner = k;
-    }
-    if ((owner < 0 ? last : owner) != (int)row.rank) return;
-    run = base;
-    owner = -1;
-    last = 0;
-    double before = base;
-    for (int w = 0; w < kSmWarps && owner < 0; w++) {
-        const double next = run + sh.warp_d[w];
-        if (sh.warp_d[w] > 0.0) {
-            last = w;
-            if (warp == w) before = run;
+        const bool hit = upto + sums[k][0] > target;
+        if (hit || sums[k][0] > 0.0) {
+            last = k;
+            base = upto;
         }
-        if (next > target) owner = w;
-        run = next;
+        if (hit) owner = k;
+        upto += sums[k][0];
     }
-    if ((owner < 0 ? last : owner) != warp) return;
-    seen = ties_before;
-    int token = -1;
-    double share_w = 0.0;
-    for (int i = i0 + lane; i - lane < i1; i += 32) {
-        const double w = kept(i, seen);
-        double upto = w;
+    if (last != (int)row.rank || warp != 0) return;
+    int q = -1, q_last = 0;
+    for (int q0 = 0; q0 < runs && q < 0; q0 += 32) {
+        const int mine = q0 + lane;
+        const double s = mine < runs ? sh.runs.sums[mine] : 0.0, s0 = mine > 0 && mine < runs ? sh.runs.sums[mine - 1] : 0.0;
+        const unsigned hit = __ballot_sync(0xffffffffu, mine < runs && base + s > target), any = __ballot_sync(0xffffffffu, mine < runs && s > s0);
+        if (any) q_last = q0 + 31 - __clz(any);
+        if (hit) q = q0 + __ffs(hit) - 1;
+    }
+    if (q < 0) q = q_last;
+    if (q > 0) base += sh.runs.sums[q - 1];
+    double w[8];
+    weigh(q, ranked ? ties_before + sh.runs.ties[q] : 0, w);
+    const double mine = ((w[0] + w[1]) + (w[2] + w[3])) + ((w[4] + w[5]) + (w[6] + w[7]));
+    double run = mine;
 #pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const double v = __shfl_up_sync(0xffffffffu, upto, o);
-            if (lane >= o) upto += v;
-        }
-        const unsigned hit = __ballot_sync(0xffffffffu, w > 0.0 && before + upto > target), any = __ballot_sync(0xffffffffu, w > 0.0);
-        if (any) {
-            const int l = hit ? __ffs(hit) - 1 : 31 - __clz(any);
-            token = row.base + i - lane + l;
-            share_w = __shfl_sync(0xffffffffu, w, l);
-        }
-        if (hit) break;
-        before += __shfl_sync(0xffffffffu, upto, 31);
+    for (int o = 1; o < 32; o <<= 1) {
+        const double v = __shfl_up_sync(0xffffffffu, run, o);
+        if (lane >= o) run += v;
     }
-    if (lane == 0) {
-        p.tokens[r] = token;
-        if (p.logprobs) p.logprobs[r] = (float)log(share_w / total);
+    const unsigned hit = __ballot_sync(0xffffffffu, mine > 0.0 && base + run > target), any = __ballot_sync(0xffffffffu, mine > 0.0);
+    if (!any || lane != (hit ? __ffs(hit) - 1 : 31 - __clz(any))) return;  // (any: the run has mass)
+    run += base - mine;
+    int at = -1;
+    double share_w = 0.0;
+    bool past = false;
+#pragma unroll
+    for (int e = 0; e < 8; e++) {
+        run += w[e];
+        if (w[e] > 0.0 && !past) {
+            at = e;
+            share_w = w[e];
+            past = run > target;
+        }
     }
+    p.tokens[r] = row.base + q * kSmRun + lane * 8 + at;
+    if (p.logprobs) p.logprobs[r] = (float)log(share_w / total);
 }
 
 }  // namespace dbt
