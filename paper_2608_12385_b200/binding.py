@@ -6,7 +6,9 @@ libdbt_b200.so.  Loading fails loudly when the library has not been built
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes as C
+import functools
 import os
 import struct
 
@@ -201,34 +203,47 @@ ROPE_KINDS = {"plain": 0, "linear": 1, "base": 2, "ramp": 3, "bands": 4}
 _DTYPES = {torch.float32: 0, torch.bfloat16: 1}
 
 
+_I32, _F32, _F64 = torch.int32, torch.float32, torch.float64
+_current_device, _current_stream = torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream
+
+
 def _need(cond, message: str):
     if not cond:
         raise DbtError(1, message)
 
 
+# The checks stand in one condition each and call _refuse for the message: a call costs a microsecond per tensor otherwise.
+def _refuse(**tensors):
+    """Say which of name = (tensor, dtype, shape) is not a contiguous tensor of that type and shape (None passes)."""
+    for name, (t, dtype, shape) in tensors.items():
+        if t is not None and not (t.dtype is dtype and t.shape == shape and t.is_contiguous()):
+            raise DbtError(1, f"{name}: contiguous {dtype} {tuple(shape)} expected, got {t.dtype} {tuple(t.shape)}")
+
+
 def _dtype(t: torch.Tensor) -> int:
-    _need(t.dtype in _DTYPES, f"float32 or bfloat16 expected, got {t.dtype}")
-    return _DTYPES[t.dtype]
+    dt = _DTYPES.get(t.dtype)
+    if dt is None:
+        raise DbtError(1, f"float32 or bfloat16 expected, got {t.dtype}")
+    return dt
 
 
-def _ints(name: str, t, shape):
-    """An int32 tensor of that shape, contiguous (None passes)."""
-    if t is not None:
-        _need(t.dtype is torch.int32 and t.shape == shape and t.is_contiguous(), f"{name}: contiguous int32 {tuple(shape)} expected")
-
-
-def _enqueue(fn, tensors, *args):
-    """Call the entry on the current stream of the device that all tensors are on."""
-    dev = tensors[0].get_device()
+def _stream(dev: int, tensors) -> int:
+    """The current stream of the device that all tensors are on."""
     for t in tensors:
         if t is not None and t.get_device() != dev:
             raise DbtError(1, "all tensors have to be on one GPU")
-    _need(dev >= 0, "the tensors have to be on a GPU")
-    if dev == torch._C._cuda_getDevice():
-        st = fn(*args, torch._C._cuda_getCurrentRawStream(dev))
+    if dev < 0:
+        raise DbtError(1, "the tensors have to be on a GPU")
+    return _current_stream(dev)
+
+
+def _call(fn, dev: int, *args):
+    """Call an entry with `dev` as the current device."""
+    if dev == _current_device():
+        st = fn(*args)
     else:
         with torch.cuda.device(dev):
-            st = fn(*args, torch._C._cuda_getCurrentRawStream(dev))
+            st = fn(*args)
     if st != DBT_OK:
         raise DbtError(st, load_library().dbt_last_error(None).decode())
 
@@ -240,16 +255,8 @@ def check_status(status: torch.Tensor):
         raise DbtError(7 if code[0] == 3 else 6, f"device status {code}")
 
 
-def _enqueue_checked(fn, tensors, status, pack):
-    """With a caller's status word the call does not wait; without one it waits and raises what the device found."""
-    own = status is None
-    if own:
-        status = torch.zeros(2, dtype=torch.int32, device=tensors[0].device)
-    else:
-        _ints("status", status, (2,))
-    _enqueue(fn, (*tensors, status), pack(status.data_ptr()))
-    if own:
-        check_status(status)
+def _own_status(like: torch.Tensor) -> torch.Tensor:
+    return torch.zeros(2, dtype=torch.int32, device=like.device)
 
 
 def rope_frequencies(rot_dim: int, base: float = 10000.0, kind: str = "plain", factor: float = 1.0, trained_len: float = 0.0,
@@ -271,29 +278,30 @@ def op_rope(x: torch.Tensor, positions: torch.Tensor, freq: torch.Tensor, scale:
             inverse: bool = False, out: torch.Tensor | None = None) -> torch.Tensor:
     """x [rows, heads, head_dim] with the first 2 * freq.numel() elements of every head rotated by positions [rows] (int32)
     times freq (float64, on x's device).  inverse: the transposed map, which is the gradient.  out may be x."""
-    L = load_library()
+    L = _lib or load_library()
     dt = _dtype(x)
-    _need(x.dim() == 3 and x.stride(2) == 1, "x: [rows, heads, head_dim] with contiguous head_dim expected")
+    _need(x.dim() == 3, "x: [rows, heads, head_dim] expected")
     rows, heads, dim = x.shape
+    xs = x.stride()
     if out is None:
         out = torch.empty((rows, heads, dim), dtype=x.dtype, device=x.device)
-    _need(out.shape == x.shape and out.dtype is x.dtype and out.stride(2) == 1, "out: x's shape and type, contiguous head_dim")
-    _ints("positions", positions, (rows,))
-    _need(freq.dtype is torch.float64 and freq.dim() == 1 and freq.is_contiguous(), "freq: contiguous float64 [rot_dim / 2] expected")
-    _enqueue(L.dbt_op_rope, (x, out, positions, freq), x.data_ptr(), out.data_ptr(), positions.data_ptr(), freq.data_ptr(), rows, heads,
-             dim, 2 * freq.numel(), x.stride(0), x.stride(1), out.stride(0), out.stride(1), scale, int(interleaved), int(inverse), dt)
+    ys = out.stride()
+    if not (xs[2] == 1 and out.dtype is x.dtype and out.shape == x.shape and ys[2] == 1):
+        raise DbtError(1, "x, out: the same shape and type with contiguous head_dim expected")
+    if not (positions.dtype is _I32 and positions.shape == (rows,) and positions.is_contiguous() and freq.dtype is _F64 and freq.dim() == 1
+            and freq.is_contiguous()):
+        _refuse(positions=(positions, _I32, (rows,)), freq=(freq, _F64, (freq.numel(),)))
+    dev = x.get_device()
+    _call(L.dbt_op_rope, dev, x.data_ptr(), out.data_ptr(), positions.data_ptr(), freq.data_ptr(), rows, heads, dim, 2 * freq.numel(), xs[0], xs[1],
+          ys[0], ys[1], scale, interleaved, inverse, dt, _stream(dev, (out, positions, freq)))
     return out
 
 
 def _cache_shape(cache: torch.Tensor, dims: int, dtype):
-    _need(cache.dim() == dims and cache.shape[-5] == 2 and cache.shape[-2] == 16 and cache.is_contiguous() and cache.dtype is dtype,
-          "cache: contiguous [.., 2, pages, kv heads, 16, head_dim] of the activations' type expected")
-    return cache.shape[-4], cache.shape[-3], cache.shape[-1]
-
-
-def _heads(name: str, t: torch.Tensor, B: int, N: int, dim: int, dtype):
-    _need(t.dim() == 4 and t.shape[0] == B and t.shape[1] == N and t.shape[3] == dim and t.stride(3) == 1 and t.dtype is dtype,
-          f"{name}: [B, nodes, heads, head_dim] of the cache's type with contiguous head_dim expected")
+    shape = cache.shape
+    if not (len(shape) == dims and shape[-5] == 2 and shape[-2] == 16 and cache.dtype is dtype and cache.is_contiguous()):
+        raise DbtError(1, "cache: contiguous [.., 2, pages, kv heads, 16, head_dim] of the activations' type expected")
+    return shape[-4], shape[-3], shape[-1]
 
 
 def op_rope_append(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, positions: torch.Tensor, freq: torch.Tensor, cache_layer: torch.Tensor,
@@ -301,34 +309,39 @@ def op_rope_append(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, positions:
                    interleaved: bool = False, out: torch.Tensor | None = None, status: torch.Tensor | None = None) -> torch.Tensor:
     """q [B, N, query heads, head_dim], k, v [B, N, kv heads, head_dim] (any strides but the last) of N nodes per sequence: q and k
     rotated by positions [B, N]; the keys and values go to cache positions seq_lens[b] + node of cache_layer [2, pages, kv heads, 16,
-    head_dim], the rotated queries are returned.  counts [B]: nodes that count; rows behind them are left as they were."""
-    L = load_library()
-    dt = _dtype(q)
-    pages, nkv, dim = _cache_shape(cache_layer, 5, q.dtype)
-    _need(q.dim() == 4, "q: [B, nodes, heads, head_dim] expected")
-    B, N, nq, _ = q.shape
-    _heads("q", q, B, N, dim, q.dtype)
-    _heads("k", k, B, N, dim, q.dtype)
-    _heads("v", v, B, N, dim, q.dtype)
-    _need(k.shape[2] == nkv and v.shape[2] == nkv, "k, v: the cache's number of heads expected")
+    head_dim], the rotated queries are returned.  counts [B]: nodes that count; rows behind them are left as they were.  With a status
+    word of the caller's (int32 [2], zeros; see check_status) the call does not wait; without one it waits and raises what the device
+    found."""
+    L = _lib or load_library()
+    dt, dtype = _dtype(q), q.dtype
+    pages, nkv, dim = _cache_shape(cache_layer, 5, dtype)
+    _need(q.dim() == 4 and page_table.dim() == 2, "q: [B, nodes, heads, head_dim], page_table: [B, pages per sequence] expected")
+    B, N, nq, qd = q.shape
+    pps = page_table.shape[1]
+    qs, ks, vs = q.stride(), k.stride(), v.stride()
+    if not (qd == dim and qs[3] == 1 and k.shape == (B, N, nkv, dim) and k.dtype is dtype and ks[3] == 1 and v.shape == (B, N, nkv, dim)
+            and v.dtype is dtype and vs[3] == 1):
+        raise DbtError(1, "q, k, v: [B, nodes, heads, head_dim] of the cache's type, head_dim and number of heads, with contiguous head_dim expected")
     if out is None:
-        out = torch.empty((B, N, nq, dim), dtype=q.dtype, device=q.device)
-    _need(out.shape == q.shape and out.dtype is q.dtype and out.is_contiguous(), "out: contiguous, q's shape and type")
-    _need(page_table.dim() == 2, "page_table: [B, pages per sequence] expected")
-    _ints("positions", positions, (B, N))
-    _ints("page_table", page_table, (B, page_table.shape[1]))
-    _ints("seq_lens", seq_lens, (B,))
-    _ints("counts", counts, (B,))
-    _need(freq.dtype is torch.float64 and freq.dim() == 1 and freq.is_contiguous(), "freq: contiguous float64 [rot_dim / 2] expected")
-
-    def pack(status_ptr):
-        return ROPE_APPEND_FORMAT.pack(
-            ROPE_APPEND_FORMAT.size, dt, B, N, nq, nkv, dim, 2 * freq.numel(), int(interleaved), pages, page_table.shape[1], scale,
-            q.data_ptr(), k.data_ptr(), v.data_ptr(), *q.stride()[:3], *k.stride()[:3], *v.stride()[:3], out.data_ptr(),
-            cache_layer.data_ptr(), positions.data_ptr(), page_table.data_ptr(), seq_lens.data_ptr(),
-            0 if counts is None else counts.data_ptr(), freq.data_ptr(), status_ptr)
-
-    _enqueue_checked(L.dbt_op_rope_append, (q, k, v, out, cache_layer, positions, page_table, seq_lens, counts, freq), status, pack)
+        out = torch.empty((B, N, nq, dim), dtype=dtype, device=q.device)
+    own = status is None
+    if own:
+        status = _own_status(q)
+    if not (out.shape == q.shape and out.dtype is dtype and out.is_contiguous() and positions.dtype is _I32 and positions.shape == (B, N)
+            and positions.is_contiguous() and page_table.dtype is _I32 and page_table.shape[0] == B and page_table.is_contiguous()
+            and seq_lens.dtype is _I32 and seq_lens.shape == (B,) and seq_lens.is_contiguous() and freq.dtype is _F64 and freq.dim() == 1
+            and freq.is_contiguous() and status.dtype is _I32 and status.shape == (2,) and status.is_contiguous()
+            and (counts is None or (counts.dtype is _I32 and counts.shape == (B,) and counts.is_contiguous()))):
+        _refuse(out=(out, dtype, q.shape), positions=(positions, _I32, (B, N)), page_table=(page_table, _I32, (B, pps)), seq_lens=(seq_lens, _I32, (B,)),
+                counts=(counts, _I32, (B,)), freq=(freq, _F64, (freq.numel(),)), status=(status, _I32, (2,)))
+    dev = q.get_device()
+    stream = _stream(dev, (k, v, out, cache_layer, positions, page_table, seq_lens, counts, freq, status))
+    _call(L.dbt_op_rope_append, dev, ROPE_APPEND_FORMAT.pack(
+        ROPE_APPEND_FORMAT.size, dt, B, N, nq, nkv, dim, 2 * freq.numel(), interleaved, pages, pps, scale, q.data_ptr(), k.data_ptr(), v.data_ptr(),
+        qs[0], qs[1], qs[2], ks[0], ks[1], ks[2], vs[0], vs[1], vs[2], out.data_ptr(), cache_layer.data_ptr(), positions.data_ptr(),
+        page_table.data_ptr(), seq_lens.data_ptr(), 0 if counts is None else counts.data_ptr(), freq.data_ptr(), status.data_ptr()), stream)
+    if own:
+        check_status(status)
     return out
 
 
@@ -337,65 +350,83 @@ def op_attn_tree(q: torch.Tensor, cache_layer: torch.Tensor, page_table: torch.T
                  workspace: torch.Tensor | None = None, status: torch.Tensor | None = None) -> torch.Tensor:
     """Attention of the N drafted nodes of every sequence: q [B, N, query heads, head_dim]; node i sees the seq_lens[b] cached positions,
     itself and its ancestors by parents [B, N] (-1: a root), whose keys and values stand in the cache behind them.  workspace (uint8, at
-    least attn_tree_workspace(...) bytes) is allocated when none is given."""
-    L = load_library()
-    dt = _dtype(q)
-    pages, nkv, dim = _cache_shape(cache_layer, 5, q.dtype)
-    _need(q.dim() == 4, "q: [B, nodes, heads, head_dim] expected")
-    B, N, nq, _ = q.shape
-    _heads("q", q, B, N, dim, q.dtype)
+    least attn_tree_workspace(...) bytes) is allocated when none is given.  status as in op_rope_append."""
+    L = _lib or load_library()
+    dt, dtype = _dtype(q), q.dtype
+    pages, nkv, dim = _cache_shape(cache_layer, 5, dtype)
+    _need(q.dim() == 4 and page_table.dim() == 2, "q: [B, nodes, heads, head_dim], page_table: [B, pages per sequence] expected")
+    B, N, nq, qd = q.shape
+    pps = page_table.shape[1]
+    qs = q.stride()
+    if qd != dim or qs[3] != 1:
+        raise DbtError(1, "q: [B, nodes, heads, head_dim] of the cache's head_dim, contiguous in it, expected")
+    dev = q.get_device()
     if out is None:
-        out = torch.empty((B, N, nq, dim), dtype=q.dtype, device=q.device)
-    _need(out.shape == q.shape and out.dtype is q.dtype and out.is_contiguous(), "out: contiguous, q's shape and type")
-    _need(page_table.dim() == 2, "page_table: [B, pages per sequence] expected")
-    _ints("page_table", page_table, (B, page_table.shape[1]))
-    _ints("seq_lens", seq_lens, (B,))
-    _ints("parents", parents, (B, N))
-    _ints("counts", counts, (B,))
+        out = torch.empty((B, N, nq, dim), dtype=dtype, device=q.device)
+    own = status is None
+    if own:
+        status = _own_status(q)
     if workspace is None:
-        workspace = torch.empty(attn_tree_workspace(q, cache_layer, page_table), dtype=torch.uint8, device=q.device)
-    _need(workspace.is_contiguous(), "workspace: contiguous expected")
-
-    def pack(status_ptr):
-        return ATTN_TREE_FORMAT.pack(
-            ATTN_TREE_FORMAT.size, dt, B, N, nq, nkv, dim, pages, page_table.shape[1], softmax_scale, q.data_ptr(), cache_layer.data_ptr(),
-            *q.stride()[:3], out.data_ptr(), page_table.data_ptr(), seq_lens.data_ptr(), 0 if counts is None else counts.data_ptr(),
-            parents.data_ptr(), workspace.data_ptr(), workspace.numel() * workspace.element_size(), status_ptr)
-
-    _enqueue_checked(L.dbt_op_attn_tree, (q, out, cache_layer, page_table, seq_lens, parents, counts, workspace), status, pack)
+        workspace = torch.empty(_tree_workspace(dt, B, N, nq, nkv, dim, pages, pps, dev), dtype=torch.uint8, device=q.device)
+    if not (out.shape == q.shape and out.dtype is dtype and out.is_contiguous() and page_table.dtype is _I32 and page_table.shape[0] == B
+            and page_table.is_contiguous() and seq_lens.dtype is _I32 and seq_lens.shape == (B,) and seq_lens.is_contiguous()
+            and parents.dtype is _I32 and parents.shape == (B, N) and parents.is_contiguous() and status.dtype is _I32 and status.shape == (2,) and status.is_contiguous()
+            and workspace.is_contiguous() and (counts is None or (counts.dtype is _I32 and counts.shape == (B,) and counts.is_contiguous()))):
+        _refuse(out=(out, dtype, q.shape), page_table=(page_table, _I32, (B, pps)), seq_lens=(seq_lens, _I32, (B,)), parents=(parents, _I32, (B, N)),
+                counts=(counts, _I32, (B,)), status=(status, _I32, (2,)), workspace=(workspace, workspace.dtype, workspace.shape))
+    stream = _stream(dev, (out, cache_layer, page_table, seq_lens, parents, counts, workspace, status))
+    _call(L.dbt_op_attn_tree, dev, ATTN_TREE_FORMAT.pack(
+        ATTN_TREE_FORMAT.size, dt, B, N, nq, nkv, dim, pages, pps, softmax_scale, q.data_ptr(), cache_layer.data_ptr(), qs[0], qs[1], qs[2],
+        out.data_ptr(), page_table.data_ptr(), seq_lens.data_ptr(), 0 if counts is None else counts.data_ptr(), parents.data_ptr(),
+        workspace.data_ptr(), workspace.numel() * workspace.element_size(), status.data_ptr()), stream)
+    if own:
+        check_status(status)
     return out
+
+
+@functools.lru_cache(maxsize=256)
+def _tree_workspace(dt: int, B: int, N: int, nq: int, nkv: int, dim: int, pages: int, pps: int, dev: int) -> int:
+    """The size that the library asks for: a function of these numbers and of the device's SMs alone."""
+    L = load_library()
+    n = C.c_size_t(0)
+    args = ATTN_TREE_FORMAT.pack(ATTN_TREE_FORMAT.size, dt, B, N, nq, nkv, dim, pages, pps, 0.0, *[0] * 13)
+    with torch.cuda.device(dev) if dev >= 0 else contextlib.nullcontext():
+        st = L.dbt_op_attn_tree_workspace(args, C.byref(n))
+    if st != DBT_OK:
+        raise DbtError(st, L.dbt_last_error(None).decode())
+    return n.value
 
 
 def attn_tree_workspace(q: torch.Tensor, cache_layer: torch.Tensor, page_table: torch.Tensor) -> int:
     """Bytes of workspace that op_attn_tree needs for tensors of these shapes."""
-    L = load_library()
     B, N, nq, dim = q.shape
-    n = C.c_size_t(0)
-    args = ATTN_TREE_FORMAT.pack(ATTN_TREE_FORMAT.size, _dtype(q), B, N, nq, cache_layer.shape[2], dim, cache_layer.shape[1], page_table.shape[1],
-                                 0.0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0)
-    st = L.dbt_op_attn_tree_workspace(args, C.byref(n))
-    if st != DBT_OK:
-        raise DbtError(st, L.dbt_last_error(None).decode())
-    return n.value
+    return _tree_workspace(_dtype(q), B, N, nq, cache_layer.shape[2], dim, cache_layer.shape[1], page_table.shape[1], q.get_device())
 
 
 def op_sample(logits: torch.Tensor, uniforms: torch.Tensor, temperature: torch.Tensor | None = None, top_k: torch.Tensor | None = None,
               top_p: torch.Tensor | None = None, min_p: torch.Tensor | None = None) -> tuple[torch.Tensor, torch.Tensor]:
     """A token per row of logits [rows, vocab] from one number in [0, 1) a row (uniforms fp32 [rows]); temperature, top_p, min_p fp32 [rows]
     and top_k int32 [rows], each optional.  Returns (tokens int32 [rows], log of each token's share of what the filters leave)."""
-    L = load_library()
+    L = _lib or load_library()
     dt = _dtype(logits)
-    _need(logits.dim() == 2 and logits.stride(1) == 1, "logits: [rows, vocab] with contiguous rows expected")
+    _need(logits.dim() == 2, "logits: [rows, vocab] expected")
     R, V = logits.shape
-    for name, t in (("uniforms", uniforms), ("temperature", temperature), ("top_p", top_p), ("min_p", min_p)):
-        if t is not None:
-            _need(t.dtype is torch.float32 and t.shape == (R,) and t.is_contiguous(), f"{name}: contiguous float32 [rows] expected")
-    _ints("top_k", top_k, (R,))
-    tokens = torch.empty(R, dtype=torch.int32, device=logits.device)
-    logprobs = torch.empty(R, dtype=torch.float32, device=logits.device)
-    _enqueue(L.dbt_op_sample, (logits, uniforms, temperature, top_k, top_p, min_p), logits.data_ptr(), dt, R, V,
-             logits.stride(0) if R > 1 else V, uniforms.data_ptr(), _p(temperature), _p(top_k), _p(top_p), _p(min_p), tokens.data_ptr(),
-             logprobs.data_ptr())
+    zs = logits.stride()
+    one = (R,)
+    if not (zs[1] == 1 and uniforms.dtype is _F32 and uniforms.shape == one and uniforms.is_contiguous()
+            and (temperature is None or (temperature.dtype is _F32 and temperature.shape == one and temperature.is_contiguous()))
+            and (top_k is None or (top_k.dtype is _I32 and top_k.shape == one and top_k.is_contiguous()))
+            and (top_p is None or (top_p.dtype is _F32 and top_p.shape == one and top_p.is_contiguous()))
+            and (min_p is None or (min_p.dtype is _F32 and min_p.shape == one and min_p.is_contiguous()))):
+        _need(zs[1] == 1, "logits: contiguous rows expected")
+        _refuse(uniforms=(uniforms, _F32, one), temperature=(temperature, _F32, one), top_k=(top_k, _I32, one), top_p=(top_p, _F32, one),
+                min_p=(min_p, _F32, one))
+    dev = logits.get_device()
+    stream = _stream(dev, (uniforms, temperature, top_k, top_p, min_p))
+    device = logits.device
+    tokens, logprobs = torch.empty(R, dtype=_I32, device=device), torch.empty(R, dtype=_F32, device=device)
+    _call(L.dbt_op_sample, dev, logits.data_ptr(), dt, R, V, zs[0] if R > 1 else V, uniforms.data_ptr(), _p(temperature), _p(top_k), _p(top_p), _p(min_p),
+          tokens.data_ptr(), logprobs.data_ptr(), stream)
     return tokens, logprobs
 
 
@@ -403,28 +434,35 @@ def op_tree_accept(tokens: torch.Tensor, parents: torch.Tensor, sampled: torch.T
                    seq_lens: torch.Tensor, counts: torch.Tensor | None = None, status: torch.Tensor | None = None):
     """The walk from node 0 along the children whose token was sampled at their parent; the accepted nodes' rows of pool [layers, 2, pages,
     kv heads, 16, head_dim] are moved together behind the cached positions.  tokens, parents, sampled [B, N] int32.  Returns (path [B, N],
-    accepted nodes [B], token sampled at the last of them [B], new lengths [B]), all int32."""
-    L = load_library()
+    accepted nodes [B], token sampled at the last of them [B], new lengths [B]), all int32.  status as in op_rope_append."""
+    L = _lib or load_library()
     dt = _dtype(pool)
     pages, nkv, dim = _cache_shape(pool, 6, pool.dtype)
     _need(tokens.dim() == 2 and page_table.dim() == 2, "tokens: [B, nodes], page_table: [B, pages per sequence] expected")
-    B, N = tokens.shape
-    _ints("tokens", tokens, (B, N))
-    _ints("parents", parents, (B, N))
-    _ints("sampled", sampled, (B, N))
-    _ints("page_table", page_table, (B, page_table.shape[1]))
-    _ints("seq_lens", seq_lens, (B,))
-    _ints("counts", counts, (B,))
-    path = torch.empty((B, N), dtype=torch.int32, device=tokens.device)
-    accepted, following, lens = torch.empty((3, B), dtype=torch.int32, device=tokens.device).unbind(0)
-
-    def pack(status_ptr):
-        return TREE_ACCEPT_FORMAT.pack(
-            TREE_ACCEPT_FORMAT.size, dt, B, N, pool.shape[0], nkv, dim, pages, page_table.shape[1], tokens.data_ptr(), parents.data_ptr(),
-            sampled.data_ptr(), page_table.data_ptr(), seq_lens.data_ptr(), 0 if counts is None else counts.data_ptr(), pool.data_ptr(),
-            path.data_ptr(), accepted.data_ptr(), following.data_ptr(), lens.data_ptr(), status_ptr)
-
-    _enqueue_checked(L.dbt_op_tree_accept, (tokens, parents, sampled, pool, page_table, seq_lens, counts), status, pack)
+    both = B, N = tokens.shape
+    pps = page_table.shape[1]
+    own = status is None
+    if own:
+        status = _own_status(tokens)
+    if not (tokens.dtype is _I32 and tokens.is_contiguous() and parents.dtype is _I32 and parents.shape == both and parents.is_contiguous()
+            and sampled.dtype is _I32 and sampled.shape == both and sampled.is_contiguous() and page_table.dtype is _I32
+            and page_table.shape[0] == B and page_table.is_contiguous() and seq_lens.dtype is _I32 and seq_lens.shape == (B,)
+            and seq_lens.is_contiguous() and status.dtype is _I32 and status.shape == (2,) and status.is_contiguous()
+            and (counts is None or (counts.dtype is _I32 and counts.shape == (B,) and counts.is_contiguous()))):
+        _refuse(tokens=(tokens, _I32, both), parents=(parents, _I32, both), sampled=(sampled, _I32, both), page_table=(page_table, _I32, (B, pps)),
+                seq_lens=(seq_lens, _I32, (B,)), counts=(counts, _I32, (B,)), status=(status, _I32, (2,)))
+    dev = tokens.get_device()
+    stream = _stream(dev, (parents, sampled, pool, page_table, seq_lens, counts, status))
+    device = tokens.device
+    path = torch.empty(both, dtype=_I32, device=device)
+    accepted, following, lens = torch.empty((3, B), dtype=_I32, device=device).unbind(0)
+    first = accepted.data_ptr()
+    _call(L.dbt_op_tree_accept, dev, TREE_ACCEPT_FORMAT.pack(
+        TREE_ACCEPT_FORMAT.size, dt, B, N, pool.shape[0], nkv, dim, pages, pps, tokens.data_ptr(), parents.data_ptr(), sampled.data_ptr(),
+        page_table.data_ptr(), seq_lens.data_ptr(), 0 if counts is None else counts.data_ptr(), pool.data_ptr(), path.data_ptr(), first,
+        first + 4 * B, first + 8 * B, status.data_ptr()), stream)
+    if own:
+        check_status(status)
     return path, accepted, following, lens
 
 

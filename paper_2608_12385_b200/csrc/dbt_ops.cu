@@ -381,13 +381,13 @@ dbt_status dbt_op_sample(const void *logits, int32_t dtype, int32_t rows, int32_
             !((long long)rows * cluster >= 2 * sms && vocab <= cluster * 16384)))
         cluster *= 2;
     p.slice = ((vocab + cluster - 1) / cluster + 7) / 8 * 8;
-    // Few rows: four times the threads, so that a pass over a block's share is a fourth as long (one block per SM then).
+    // Few rows: twice the threads, one block per SM: top-k 2000 of one row of 128256 62 us with 256 threads, 52 with 512 (1024 spill: 60).
     const bool few = (long long)rows * cluster <= sms;
     cudaError_t e;
     if (dtype == DBT_DTYPE_F32)
-        e = few ? sample_launch<float, 1024>(p, rows, cluster, cuda_stream) : sample_launch<float, 256>(p, rows, cluster, cuda_stream);
+        e = few ? sample_launch<float, 512>(p, rows, cluster, cuda_stream) : sample_launch<float, 256>(p, rows, cluster, cuda_stream);
     else
-        e = few ? sample_launch<__nv_bfloat16, 1024>(p, rows, cluster, cuda_stream) : sample_launch<__nv_bfloat16, 256>(p, rows, cluster, cuda_stream);
+        e = few ? sample_launch<__nv_bfloat16, 512>(p, rows, cluster, cuda_stream) : sample_launch<__nv_bfloat16, 256>(p, rows, cluster, cuda_stream);
     return launched(e, "sample");
 }
 

@@ -123,7 +123,7 @@ struct SampleRow {
     // several in flight, and the single values before the first whole vector and after the last.
     template <typename F>
     __device__ __forceinline__ void each(F f) const {
-        constexpr int VN = 16 / sizeof(T), A = sizeof(T) == 4 ? 8 : 4;
+        constexpr int VN = 16 / sizeof(T), A = 4;
         const int tid = threadIdx.x, lead = min(n, (int)((16 - (reinterpret_cast<uintptr_t>(src) & 15)) & 15) / (int)sizeof(T));
         const int vecs = (n - lead) / VN, tail = lead + vecs * VN;
         const uint4 *v = reinterpret_cast<const uint4 *>(src + lead);
