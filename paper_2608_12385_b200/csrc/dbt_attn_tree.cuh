@@ -51,35 +51,30 @@ template <int ROWS, int KEYS>
 struct TreePlan {
     static __device__ __forceinline__ int tiles(const TreeSeq &s) { return s.n > 0 ? (s.len + s.n + KEYS - 1) / KEYS : 0; }
     static __device__ __forceinline__ int row_blocks(const TreeAttnParams &p, const TreeSeq &s) { return (s.n * p.G + ROWS - 1) / ROWS; }
-    static __device__ __forceinline__ long long units(const TreeAttnParams &p, int b) {
+    static __device__ __forceinline__ int units(const TreeAttnParams &p, int b) {  // (the host has checked that the line fits 31 bits)
         const TreeSeq s = tree_seq(p, b);
-        return s.n > 0 ? (long long)(tiles(s) + p.lead) * row_blocks(p, s) * p.hkv : 0;
-    }
-    static __device__ __forceinline__ long long warp_total(long long v) {
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-        return v;
+        return s.n > 0 ? (tiles(s) + p.lead) * row_blocks(p, s) * p.hkv : 0;
     }
     // By a whole warp: all units, and of sequence `upto` those before it.
-    static __device__ __forceinline__ long long total(const TreeAttnParams &p, int lane, int upto, long long *before) {
-        long long sum = 0, part = 0;
+    static __device__ __forceinline__ int total(const TreeAttnParams &p, int lane, int upto, int *before) {
+        int sum = 0, part = 0;
         for (int b = lane; b < p.B; b += 32) {
-            const long long u = units(p, b);
+            const int u = units(p, b);
             sum += u;
             if (b < upto) part += u;
         }
-        if (before) *before = warp_total(part);
-        return warp_total(sum);
+        if (before) *before = __reduce_add_sync(0xffffffffu, part);
+        return __reduce_add_sync(0xffffffffu, sum);
     }
     // By a whole warp: the sequence that unit `at` (< total) lies in, and the units before it.
-    static __device__ __forceinline__ int locate(const TreeAttnParams &p, int lane, long long at, long long *before) {
-        long long base = 0;
+    static __device__ __forceinline__ int locate(const TreeAttnParams &p, int lane, int at, int *before) {
+        int base = 0;
         for (int b0 = 0; b0 < p.B; b0 += 32) {
-            const long long mine = b0 + lane < p.B ? units(p, b0 + lane) : 0;
-            long long run = mine;
+            const int mine = b0 + lane < p.B ? units(p, b0 + lane) : 0;
+            int run = mine;
 #pragma unroll
             for (int o = 1; o < 32; o <<= 1) {
-                const long long x = __shfl_up_sync(0xffffffffu, run, o);
+                const int x = __shfl_up_sync(0xffffffffu, run, o);
                 if (lane >= o) run += x;
             }
             const unsigned past = __ballot_sync(0xffffffffu, base + run > at);
@@ -92,36 +87,37 @@ struct TreePlan {
         }
         return p.B;
     }
-    static __device__ __forceinline__ long long per_block(const TreeAttnParams &p, long long all) { return (all + p.blocks - 1) / p.blocks; }
+    static __device__ __forceinline__ int per_block(const TreeAttnParams &p, int all) { return all / p.blocks + (all % p.blocks != 0); }
 };
 // Walks the items of a block's run of units.
 template <int ROWS, int KEYS>
 struct TreeWalk {
     using Plan = TreePlan<ROWS, KEYS>;
-    long long end, item0;  // end of the run; the current item's first unit
+    int end, item0;        // end of the run; the current item's first unit
     int b, rb, h;          // current item
     TreeSeq s;
     int tiles, t0, t1, slot;  // the item's tiles, those of this run, the workspace slot (-1: the whole item is here)
     // False where the run holds no tile.
     __device__ __forceinline__ bool start(const TreeAttnParams &p, int lane) {
-        const long long all = Plan::total(p, lane, 0, nullptr), per = Plan::per_block(p, all), at = (long long)blockIdx.x * per;
-        end = min(all, at + per);
-        if (at >= end) return false;
-        long long before;
+        const int all = Plan::total(p, lane, 0, nullptr), per = Plan::per_block(p, all);
+        if (all == 0 || (int)blockIdx.x > (all - 1) / per) return false;
+        const int at = (int)blockIdx.x * per;
+        end = at + min(per, all - at);
+        int before;
         b = Plan::locate(p, lane, at, &before);
         s = tree_seq(p, b, true);
         tiles = Plan::tiles(s);
-        const int units = tiles + p.lead, item = (int)((at - before) / units), rbs = Plan::row_blocks(p, s);
+        const int units = tiles + p.lead, item = (at - before) / units, rbs = Plan::row_blocks(p, s);
         h = item / rbs;
         rb = item - h * rbs;
-        item0 = before + (long long)item * units;
+        item0 = before + item * units;
         return place(p, at) || next(p);
     }
     // The tiles of the current item in the run's part of it, from unit `at` on.
-    __device__ __forceinline__ bool place(const TreeAttnParams &p, long long at) {
-        const long long first = item0 + p.lead;
-        t0 = (int)max(0ll, at - first);
-        t1 = (int)min((long long)tiles, end - first);
+    __device__ __forceinline__ bool place(const TreeAttnParams &p, int at) {
+        const int first = item0 + p.lead;
+        t0 = max(0, at - first);
+        t1 = min(tiles, end - first);
         // at most two items of a run are cut: the one it begins inside, the one it ends inside
         slot = t0 == 0 && t1 == tiles ? -1 : 2 * (int)blockIdx.x + (t0 == 0);
         return t1 > t0;
@@ -345,64 +341,99 @@ __global__ void __launch_bounds__(256, TreeSimtCfg<D, RM>::kBlocksPerSm) attn_tr
 // values of the nodes, once in shared memory, are looked through: elements that are not finite are replaced by 0 there, and
 // the rows that do see the node add them at the end.  Slots behind the last node are cleared the same way.
 //
-// Roles: warps 0..3, 4..7 softmax, 8 TMA, 9 MMA and tensor memory.  All waits are bounded.
+// Roles: warps 0..3, 4..7 softmax, 8 TMA, 9 MMA and tensor memory, 10 and 11 queries, parents and the look through the values.
+// An item's queries are loaded, and its first scores formed, while the softmax warps write the output of the item before.
+// All waits are bounded.
 template <int DH, bool PAIR>
 struct TreeMmaCfg {
     static constexpr int kRows = PAIR ? 256 : 128;
     static constexpr int kKeys = 128;
-    static constexpr int kThreads = 320;
+    static constexpr int kThreads = 384;
     static constexpr int kHalves = DH / 64;
     static constexpr int kTileBytes = 128 * DH * 2;  // 128 rows of queries, keys or values
     static constexpr int kQTiles = PAIR ? 2 : 1;
-    static constexpr int kStages = DH == 128 ? (PAIR ? 2 : 3) : 5;
-    static constexpr int kSmemBytes = (kQTiles + 2 * kStages) * kTileBytes + 1024 + 256;
+    static constexpr int kStagesK = DH == 128 ? 3 : 5, kStagesV = DH == 128 ? (PAIR ? 2 : 3) : 5;
+    static constexpr int kTail = 2048 + 128 + 64 + 512;  // statistics, parents, flags, barriers
+    static constexpr int kSmemBytes = (kQTiles + kStagesK + kStagesV) * kTileBytes + kTail;
     static constexpr int kTmemCols = 512;
-    static_assert(kSmemBytes + 1024 <= 227 * 1024, "shared memory of one SM");
+    static_assert(kSmemBytes <= 227 * 1024, "shared memory of one SM");
+    static_assert(8 * (2 * kStagesK + 3 * kStagesV + 11) + 4 <= 512, "barrier area");
 };
 constexpr float kTreeRescaleLog2 = 8.f;
 
+__device__ __forceinline__ uint64_t pack_f32x2(float a, float b) { return (uint64_t)__float_as_uint(b) << 32 | __float_as_uint(a); }
+__device__ __forceinline__ uint64_t fma_f32x2(uint64_t a, uint64_t b, uint64_t c) {
+    uint64_t d;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+    return d;
+}
+__device__ __forceinline__ uint64_t add_f32x2(uint64_t a, uint64_t b) {
+    uint64_t d;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+    return d;
+}
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    float d;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+    return d;
+}
+__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t *r) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};" ::"r"(taddr),
+        "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]),
+        "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
+        : "memory");
+}
+__device__ __forceinline__ void mbar_arrive(uint32_t bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory"); }
+
 template <int DH, bool PAIR>
-__global__ void __launch_bounds__(320, 1) attn_tree_mma_kernel(const __grid_constant__ CUtensorMap tmKV, const TreeAttnParams p) {
+__global__ void __launch_bounds__(384, 1) attn_tree_mma_kernel(const __grid_constant__ CUtensorMap tmKV, const TreeAttnParams p) {
     using Cfg = TreeMmaCfg<DH, PAIR>;
-    constexpr int STAGES = Cfg::kStages, HALVES = Cfg::kHalves, KS = DH / 16, KEYS = Cfg::kKeys, ROWS = Cfg::kRows;
+    constexpr int SK = Cfg::kStagesK, SV = Cfg::kStagesV, HALVES = Cfg::kHalves, KS = DH / 16, KEYS = Cfg::kKeys, ROWS = Cfg::kRows;
     constexpr uint32_t kHalfBytes = 128 * 128;  // queries: 128 rows of one 64-column piece
     constexpr uint32_t kGroup = HALVES * 1024;  // keys, values: 8 rows, their 64-column pieces one after the other
-    extern __shared__ uint8_t smem_raw[];
-    __shared__ int parents_s[2][64];
-    __shared__ unsigned long long bad_s;
-    __shared__ int failed_s;
-    const uint32_t raw = smem_u32(smem_raw);
-    const uint32_t q_s = (raw + 1023u) & ~1023u, k_s = q_s + Cfg::kQTiles * Cfg::kTileBytes, v_s = k_s + STAGES * Cfg::kTileBytes;
-    const uint32_t bars = v_s + STAGES * Cfg::kTileBytes;
+    extern __shared__ __align__(1024) uint8_t smem_raw[];
+    const uint32_t q_s = smem_u32(smem_raw), k_s = q_s + Cfg::kQTiles * Cfg::kTileBytes, v_s = k_s + SK * Cfg::kTileBytes;
+    uint8_t *tail = smem_raw + (Cfg::kQTiles + SK + SV) * Cfg::kTileBytes;
+    float2(*stats_s)[128] = reinterpret_cast<float2(*)[128]>(tail);                  // the groups' maxima and sums
+    signed char(*parents_s)[64] = reinterpret_cast<signed char(*)[64]>(tail + 2048);     // parents, two items
+    unsigned long long *bad_s = reinterpret_cast<unsigned long long *>(tail + 2176);  // nodes with values that are not finite, two items
+    int *failed_s = reinterpret_cast<int *>(tail + 2192);
+    const uint32_t bars = smem_u32(tail + 2240);
     auto k_full = [&](int s) { return bars + 8u * s; };
-    auto k_empty = [&](int s) { return bars + 8u * (STAGES + s); };
-    auto v_full = [&](int s) { return bars + 8u * (2 * STAGES + s); };
-    auto v_empty = [&](int s) { return bars + 8u * (3 * STAGES + s); };
-    auto q_full = [&](int i) { return bars + 8u * (4 * STAGES + i); };
-    auto s_full = [&](int i) { return bars + 8u * (4 * STAGES + 2 + i); };
-    auto p_full = [&](int i) { return bars + 8u * (4 * STAGES + 4 + i); };
-    auto o_full = [&](int i) { return bars + 8u * (4 * STAGES + 6 + i); };
-    uint32_t *tmem_holder = reinterpret_cast<uint32_t *>(smem_raw + (bars - raw) + 8 * (4 * STAGES + 8));
-    static_assert(8 * (4 * STAGES + 8) + 4 <= 256, "barrier area");
-
-    // the groups' maxima and sums, in the queries' place: both groups write them when all products of the item are done
-    float2(*stats_s)[128] = reinterpret_cast<float2(*)[128]>(smem_raw + (q_s - raw));
+    auto k_empty = [&](int s) { return bars + 8u * (SK + s); };
+    auto v_full = [&](int s) { return bars + 8u * (2 * SK + s); };
+    auto v_empty = [&](int s) { return bars + 8u * (2 * SK + SV + s); };
+    auto v_clean = [&](int s) { return bars + 8u * (2 * SK + 2 * SV + s); };  // looked through
+    const uint32_t more = bars + 8u * (2 * SK + 3 * SV);
+    auto s_full = [&](int i) { return more + 8u * i; };
+    auto p_full = [&](int i) { return more + 8u * (2 + i); };
+    auto o_full = [&](int i) { return more + 8u * (4 + i); };
+    auto q_full = [&](int n) { return more + 8u * (6 + (n & 1)); };  // item n's queries and parents
+    auto e_done = [&](int n) { return more + 8u * (8 + (n & 1)); };  // item n's output has been read by all softmax warps
+    const uint32_t q_empty = more + 8u * 10;                         // all products with the queries are done
+    uint32_t *tmem_holder = reinterpret_cast<uint32_t *>(tail + 2240 + 8 * (2 * SK + 3 * SV + 11));
 
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     if (tid == 0) {
-        for (int s = 0; s < STAGES; s++) {
+        for (int s = 0; s < SK; s++) {
             mbar_init(k_full(s), 1);
             mbar_init(k_empty(s), 1);
+        }
+        for (int s = 0; s < SV; s++) {
             mbar_init(v_full(s), 1);
             mbar_init(v_empty(s), 1);
+            mbar_init(v_clean(s), 2);
         }
         for (int i = 0; i < 2; i++) {
-            mbar_init(q_full(i), PAIR ? 4 : 8);
             mbar_init(s_full(i), 1);
             mbar_init(p_full(i), 4);
-            mbar_init(o_full(i), 2);  // the tensor cores are done; the nodes' values have been looked through
+            mbar_init(o_full(i), 2);  // the tensor cores are done; the issuer passes on what it knows of the values
+            mbar_init(q_full(i), 2);
+            mbar_init(e_done(i), 8);
         }
-        failed_s = 0;
+        mbar_init(q_empty, 1);
+        *failed_s = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == 9) {
@@ -420,8 +451,16 @@ __global__ void __launch_bounds__(320, 1) attn_tree_mma_kernel(const __grid_cons
     pdl_launch_dependents();  // (the joining kernel waits for this one before it reads anything)
 
     TreeWalk<ROWS, KEYS> w;
-    const bool work = w.start(p, lane);
+    const bool aligned = (q_s & 1023u) == 0;  // (dynamic shared memory begins the block's: always)
+    if (!aligned && tid == 0) report(p.status, kStatusWaitExpired, 940);
+    const bool work = aligned && w.start(p, lane);
     bool ok = true;
+    // waits of a whole warp, its first lane looking
+    auto wait = [&](uint32_t bar, int parity) {
+        bool r = true;
+        if (lane == 0) r = mbar_wait(bar, parity & 1);
+        return (bool)__shfl_sync(0xffffffffu, r, 0);
+    };
     if (work && warp == 8) {
         // ---- TMA: lane l brings page l of the tile
         if (lane == 0) tma_prefetch_desc(&tmKV);
@@ -434,30 +473,29 @@ __global__ void __launch_bounds__(320, 1) attn_tree_mma_kernel(const __grid_cons
             const bool loads = lane < 8;
             int page = loads && w.t0 * 8 + lane < pages_total ? tree_page(p, w.b, w.t0 * 8 + lane) : 0;
             for (int t = w.t0; t < w.t1 && ok; t++, c++) {
-                const int s = c % STAGES, np = min(8, pages_total - t * 8);
+                const int sk = c % SK, sv = c % SV, np = min(8, pages_total - t * 8);
                 const int row = (int)(((long long)page * p.hkv + w.h) * 2);  // in groups of 8 rows
-                const uint32_t off = s * Cfg::kTileBytes + lane * 2 * kGroup;
-                auto load = [&](uint32_t base, uint32_t bar, long long row0) {
+                auto load = [&](uint32_t dst, uint32_t bar, long long row0) {
                     if (!(loads && lane < np)) return;
                     const int at = (int)(row0 / 8) + row;
-                    if (reread) tma_load_4d(base + off, &tmKV, bar, 0, 0, 0, at);
-                    else tma_load_4d_hint(base + off, &tmKV, bar, 0, 0, 0, at, once);
+                    if (reread) tma_load_4d(dst + lane * 2 * kGroup, &tmKV, bar, 0, 0, 0, at);
+                    else tma_load_4d_hint(dst + lane * 2 * kGroup, &tmKV, bar, 0, 0, 0, at, once);
                 };
                 const int nx = (t + 1) * 8 + lane;
                 const int next_page = loads && t + 1 < w.t1 && nx < pages_total ? tree_page(p, w.b, nx) : 0;
                 if (lane == 0) {
-                    if (c >= STAGES) ok = mbar_wait(k_empty(s), ((c / STAGES) - 1) & 1);
-                    if (ok) mbar_expect_tx(k_full(s), (uint32_t)np * HALVES * 2048);
+                    if (c >= SK) ok = mbar_wait(k_empty(sk), ((c / SK) - 1) & 1);
+                    if (ok) mbar_expect_tx(k_full(sk), (uint32_t)np * HALVES * 2048);
                 }
                 ok = __shfl_sync(0xffffffffu, ok, 0);
-                if (ok) load(k_s, k_full(s), 0);
+                if (ok) load(k_s + sk * Cfg::kTileBytes, k_full(sk), 0);
                 nk += ok;
                 if (lane == 0 && ok) {
-                    if (c >= STAGES) ok = mbar_wait(v_empty(s), ((c / STAGES) - 1) & 1);
-                    if (ok) mbar_expect_tx(v_full(s), (uint32_t)np * HALVES * 2048);
+                    if (c >= SV) ok = mbar_wait(v_empty(sv), ((c / SV) - 1) & 1);
+                    if (ok) mbar_expect_tx(v_full(sv), (uint32_t)np * HALVES * 2048);
                 }
                 ok = __shfl_sync(0xffffffffu, ok, 0);
-                if (ok) load(v_s, v_full(s), v_row0);
+                if (ok) load(v_s + sv * Cfg::kTileBytes, v_full(sv), v_row0);
                 nv += ok;
                 page = next_page;
             }
@@ -465,217 +503,210 @@ __global__ void __launch_bounds__(320, 1) attn_tree_mma_kernel(const __grid_cons
         if (!ok && lane == 0) report(p.status, kStatusWaitExpired, 900);
         // the last loads have landed before the block leaves, also where a wait ran out
         if (lane == 0) {
-            for (int j = max(0, nk - STAGES); j < nk; j++) mbar_wait(k_full(j % STAGES), (j / STAGES) & 1, kWaitCycles / STAGES);
-            for (int j = max(0, nv - STAGES); j < nv; j++) mbar_wait(v_full(j % STAGES), (j / STAGES) & 1, kWaitCycles / STAGES);
+            for (int j = max(0, nk - SK); j < nk; j++) mbar_wait(k_full(j % SK), (j / SK) & 1, kWaitCycles / SK);
+            for (int j = max(0, nv - SV); j < nv; j++) mbar_wait(v_full(j % SV), (j / SV) & 1, kWaitCycles / SV);
         }
     } else if (work && warp == 9) {
-        // ---- MMA issuer (lane 0; the whole warp looks through the nodes' values)
+        // ---- MMA issuer (lane 0)
         constexpr uint32_t idesc_qk = umma_idesc(KEYS);
         constexpr uint32_t idesc_pv = umma_idesc(DH) | (1u << 16);  // B is MN-major
-        auto wait = [&](uint32_t bar, int parity) {
-            bool r = true;
-            if (lane == 0) r = mbar_wait(bar, parity & 1);
-            r = __shfl_sync(0xffffffffu, r, 0);
+        auto arrive_after = [&](uint32_t bar, int parity) {
+            const bool r = wait(bar, parity);
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
             return r;
         };
         auto qk = [&](int i, int c) {
             if (lane != 0) return;
-            const int s = c % STAGES;
 #pragma unroll
             for (int k = 0; k < KS; k++) {
                 const int h = k >> 2;
                 umma_f16(t_s(i), umma_smem_desc(q_s + (PAIR ? i : 0) * Cfg::kTileBytes + h * kHalfBytes) + 2 * (k & 3),
-                         umma_smem_desc_groups(k_s + s * Cfg::kTileBytes + h * 1024, kGroup, 0) + 2 * (k & 3), idesc_qk, k != 0);
+                         umma_smem_desc_groups(k_s + (c % SK) * Cfg::kTileBytes + h * 1024, kGroup, 0) + 2 * (k & 3), idesc_qk, k != 0);
             }
             umma_commit(s_full(i));
         };
         auto pv = [&](int i, int c, bool add) {
             if (lane != 0) return;
-            const uint64_t vd = umma_smem_desc_groups(v_s + (c % STAGES) * Cfg::kTileBytes, kGroup, 1024);
+            const uint64_t vd = umma_smem_desc_groups(v_s + (c % SV) * Cfg::kTileBytes, kGroup, 1024);
 #pragma unroll
             for (int k = 0; k < KEYS / 16; k++) umma_f16_ts(t_o(i), t_s(i) + 8 * k, vd + (2 * kGroup >> 4) * k, idesc_pv, add || k != 0);
         };
+        auto commit = [&](uint32_t bar) {
+            if (lane == 0) umma_commit(bar);
+        };
         auto done = [&](int i) {
-            if (lane != 0) return;
-            umma_commit(o_full(i));
-            asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(o_full(i)) : "memory");
+            commit(o_full(i));
+            if (lane == 0) mbar_arrive(o_full(i));
         };
-        unsigned long long bad = 0;
-        // values of tile t in stage s: clears what lies behind the last node, takes out node values that are not finite
-        auto look = [&](int t, int s) {
-            const int key0 = t * KEYS, first = max(0, w.s.len - key0), keys = min(KEYS, w.s.len + w.s.n - key0);
-            if (first >= KEYS) return;
-            auto at = [&](int chunk) {  // address of the chunk-th 16 bytes of the rows (and pieces) in order
-                const int row = chunk / (8 * HALVES), rest = chunk - row * (8 * HALVES);
-                return v_s + s * Cfg::kTileBytes + (row >> 3) * kGroup + (rest >> 3) * 1024 + (row & 7) * 128 + (rest & 7) * 16;
-            };
-            for (int i = keys * 8 * HALVES + lane; i < KEYS * 8 * HALVES; i += 32)
-                asm volatile("st.shared.v4.b32 [%0], {%1,%1,%1,%1};" ::"r"(at(i)), "r"(0u) : "memory");
-            uint32_t any = 0;
-#pragma unroll 8
-            for (int i = first * 8 * HALVES + lane; i < keys * 8 * HALVES; i += 32) {
-                uint32_t x[4];
-                asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(x[0]), "=r"(x[1]), "=r"(x[2]), "=r"(x[3]) : "r"(at(i)));
-                // an exponent of ones carries into the sign's place when one is added to it (the sign itself masked off)
-#pragma unroll
-                for (int k = 0; k < 4; k++) any |= (x[k] & 0x7f807f80u) + 0x00800080u;
-            }
-            if (__any_sync(0xffffffffu, any & 0x80008000u)) {  // rare
-                for (int i = first * 8 * HALVES + lane; i - lane < keys * 8 * HALVES; i += 32) {
-                    const bool in = i < keys * 8 * HALVES;
-                    bool found = false;
-                    if (in) {
-                        uint32_t x[4];
-                        asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(x[0]), "=r"(x[1]), "=r"(x[2]), "=r"(x[3]) : "r"(at(i)));
-#pragma unroll
-                        for (int k = 0; k < 4; k++) {
-                            if ((x[k] & 0x7f80u) == 0x7f80u) x[k] &= 0xffff0000u, found = true;
-                            if ((x[k] & 0x7f800000u) == 0x7f800000u) x[k] &= 0xffffu, found = true;
-                        }
-                        if (found) asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(at(i)), "r"(x[0]), "r"(x[1]), "r"(x[2]), "r"(x[3]) : "memory");
-                    }
-                    for (unsigned m = __ballot_sync(0xffffffffu, found); m; m &= m - 1)
-                        bad |= 1ull << (key0 + (i - lane + __ffs(m) - 1) / (8 * HALVES) - w.s.len);
-                }
-            }
-            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-            __syncwarp();
-        };
-        int c = 0, qn = 0, pn[2] = {0, 0};
+        int c = 0, n = 0, pn[2] = {0, 0};
         do {
             const int T = w.t1 - w.t0, rows = min(ROWS, w.s.n * p.G - w.rb * ROWS);
-            const int groups = PAIR ? (rows > 128 ? 2 : 1) : 1;  // PAIR: groups with rows
-            bad = 0;
-            // (PAIR: also a group without rows says that it is done with the item before)
-            for (int i = 0; i < (PAIR ? 2 : 1) && ok; i++) ok = wait(q_full(i), qn);
-            qn++;
+            const int groups = PAIR && rows > 128 ? 2 : 1;  // PAIR: groups with rows
+            ok = arrive_after(q_full(n), n >> 1);
             if (PAIR) {
-                ok = ok && wait(k_full(c % STAGES), c / STAGES);
-                if (ok) {
-                    for (int i = 0; i < groups; i++) qk(i, c);
-                    if (lane == 0) umma_commit(k_empty(c % STAGES));
-                }
+                ok = ok && arrive_after(k_full(c % SK), c / SK);
+                if (!ok) break;
+                for (int i = 0; i < groups; i++) qk(i, c);
+                commit(k_empty(c % SK));
+                if (T == 1) commit(q_empty);
+                if (n > 0) ok = arrive_after(e_done(n - 1), (n - 1) >> 1);  // the output's place is free
                 for (int t = 0; t < T && ok; t++, c++) {
-                    if (t + 1 < T) ok = wait(k_full((c + 1) % STAGES), (c + 1) / STAGES);
-                    ok = ok && wait(v_full(c % STAGES), c / STAGES);
-                    if (!ok) break;
-                    look(w.t0 + t, c % STAGES);
+                    if (t + 1 < T) ok = arrive_after(k_full((c + 1) % SK), (c + 1) / SK);
+                    ok = ok && arrive_after(v_clean(c % SV), c / SV);
                     for (int i = 0; i < groups && ok; i++) {
-                        ok = wait(p_full(i), pn[i]++);
+                        ok = arrive_after(p_full(i), pn[i]++);
                         if (!ok) break;
                         pv(i, c, t > 0);
-                        if (t + 1 < T) {
-                            qk(i, c + 1);
-                        } else {
-                            if (lane == 0) bad_s = bad;
-                            done(i);
-                        }
+                        if (t + 1 < T) qk(i, c + 1);
+                        else done(i);
                     }
-                    if (lane == 0 && ok) {
-                        umma_commit(v_empty(c % STAGES));
-                        if (t + 1 < T) umma_commit(k_empty((c + 1) % STAGES));
-                    }
+                    if (!ok) break;
+                    commit(v_empty(c % SV));
+                    if (t + 1 < T) commit(k_empty((c + 1) % SK));
+                    if (t + 2 == T) commit(q_empty);
                 }
             } else {
                 for (int t = 0; t < min(2, T) && ok; t++) {
-                    ok = wait(k_full((c + t) % STAGES), (c + t) / STAGES);
+                    ok = arrive_after(k_full((c + t) % SK), (c + t) / SK);
                     if (!ok) break;
                     qk(t, c + t);
-                    if (lane == 0) umma_commit(k_empty((c + t) % STAGES));
+                    commit(k_empty((c + t) % SK));
                 }
+                if (ok && T <= 2) commit(q_empty);
+                if (ok && n > 0) ok = arrive_after(e_done(n - 1), (n - 1) >> 1);  // the outputs' place is free
                 for (int t = 0; t < T && ok; t++, c++) {
                     const int i = t & 1;
-                    ok = wait(v_full(c % STAGES), c / STAGES);
-                    if (!ok) break;
-                    look(w.t0 + t, c % STAGES);
-                    ok = wait(p_full(i), pn[i]++);
+                    ok = arrive_after(v_clean(c % SV), c / SV) && arrive_after(p_full(i), pn[i]++);
                     if (!ok) break;
                     pv(i, c, t > 1);
-                    if (lane == 0) umma_commit(v_empty(c % STAGES));
+                    commit(v_empty(c % SV));
                     if (t + 2 < T) {
-                        ok = wait(k_full((c + 2) % STAGES), (c + 2) / STAGES);
+                        ok = arrive_after(k_full((c + 2) % SK), (c + 2) / SK);
                         if (!ok) break;
                         qk(i, c + 2);
-                        if (lane == 0) umma_commit(k_empty((c + 2) % STAGES));
+                        commit(k_empty((c + 2) % SK));
+                        if (t + 3 == T) commit(q_empty);
                     } else {
-                        if (lane == 0 && t == T - 1) bad_s = bad;
                         done(i);
                     }
                 }
             }
+            n++;
         } while (ok && w.next(p));
         if (!ok && lane == 0) report(p.status, kStatusWaitExpired, 910);
-    } else if (work && warp < 8) {
+    } else if (work && warp >= 10) {
+        // ---- queries, parents, values that are not finite: 64 threads
+        const int x = tid - 320;
+        const __nv_bfloat16 *q = reinterpret_cast<const __nv_bfloat16 *>(p.q);
+        int c = 0, n = 0;
+        do {
+            const int row0 = w.rb * ROWS, rows = min(ROWS, w.s.n * p.G - row0);
+            const int parent = x < w.s.n ? p.parents[(size_t)w.b * p.N + x] : -1;
+            if (n > 1) ok = wait(e_done(n - 2), (n - 2) >> 1);  // the buffers of the item before the last are free
+            if (ok && n > 0) ok = wait(q_empty, n - 1);
+            if (!ok) break;
+            constexpr int CH = DH / 8, LOADS = Cfg::kQTiles * 128 * CH / 64, BATCH = 4;
+            for (int l0 = 0; l0 < LOADS; l0 += BATCH) {
+                uint4 v[BATCH];
+#pragma unroll
+                for (int l = 0; l < BATCH; l++) {
+                    const int idx = x + (l0 + l) * 64, row = idx / CH, ch = idx - row * CH;
+                    v[l] = make_uint4(0, 0, 0, 0);
+                    if (row < rows) {
+                        const int node = (row0 + row) / p.G, g = (row0 + row) - node * p.G;
+                        const __nv_bfloat16 *src = q + w.b * p.qs[0] + node * p.qs[1] + (w.h * p.G + g) * p.qs[2] + ch * 8;
+                        if (p.q_vectors) {
+                            v[l] = __ldg(reinterpret_cast<const uint4 *>(src));
+                        } else {
+                            uint32_t y[4];
+#pragma unroll
+                            for (int k = 0; k < 4; k++)
+                                y[k] = (uint32_t)__bfloat16_as_ushort(src[2 * k]) | ((uint32_t)__bfloat16_as_ushort(src[2 * k + 1]) << 16);
+                            v[l] = make_uint4(y[0], y[1], y[2], y[3]);
+                        }
+                    }
+                }
+#pragma unroll
+                for (int l = 0; l < BATCH; l++) {
+                    const int idx = x + (l0 + l) * 64, row = idx / CH, ch = idx - row * CH;
+                    asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(q_s + (row >> 7) * Cfg::kTileBytes + (ch >> 3) * kHalfBytes +
+                                                                               (row & 127) * 128 + (((ch & 7) ^ (row & 7)) << 4)),
+                                 "r"(v[l].x), "r"(v[l].y), "r"(v[l].z), "r"(v[l].w)
+                                 : "memory");
+                }
+            }
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            // a bad parent counts as none
+            if (x < w.s.n && (parent >= x || parent < -1)) report(p.status, kStatusBadTree, parent);
+            parents_s[n & 1][x] = (signed char)(parent >= x || parent < -1 ? -1 : parent);
+            if (x == 0) bad_s[n & 1] = 0;
+            asm volatile("bar.sync 2, 64;" ::: "memory");  // (both warps: bad_s is cleared before either marks a node)
+            if (lane == 0) mbar_arrive(q_full(n));
+            for (int t = w.t0; t < w.t1 && ok; t++, c++) {
+                const int sv = c % SV;
+                ok = wait(v_full(sv), c / SV);
+                if (!ok) break;
+                const int key0 = t * KEYS, first = max(0, w.s.len - key0), keys = min(KEYS, w.s.len + w.s.n - key0);
+                if (first < KEYS) {
+                    auto at = [&](int chunk) {  // address of the chunk-th 16 bytes of the rows (and pieces) in order
+                        const int row = chunk / (8 * HALVES), rest = chunk - row * (8 * HALVES);
+                        return v_s + sv * Cfg::kTileBytes + (row >> 3) * kGroup + (rest >> 3) * 1024 + (row & 7) * 128 + (rest & 7) * 16;
+                    };
+                    for (int i = keys * 8 * HALVES + x; i < KEYS * 8 * HALVES; i += 64)
+                        asm volatile("st.shared.v4.b32 [%0], {%1,%1,%1,%1};" ::"r"(at(i)), "r"(0u) : "memory");
+                    uint32_t any = 0;
+#pragma unroll 8
+                    for (int i = first * 8 * HALVES + x; i < keys * 8 * HALVES; i += 64) {
+                        uint32_t y[4];
+                        asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(y[0]), "=r"(y[1]), "=r"(y[2]), "=r"(y[3]) : "r"(at(i)));
+                        // an exponent of ones carries into the sign's place when one is added to it (the sign itself masked off)
+#pragma unroll
+                        for (int k = 0; k < 4; k++) any |= (y[k] & 0x7f807f80u) + 0x00800080u;
+                    }
+                    if (any & 0x80008000u) {  // rare
+                        for (int i = first * 8 * HALVES + x; i < keys * 8 * HALVES; i += 64) {
+                            uint32_t y[4];
+                            bool found = false;
+                            asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(y[0]), "=r"(y[1]), "=r"(y[2]), "=r"(y[3]) : "r"(at(i)));
+#pragma unroll
+                            for (int k = 0; k < 4; k++) {
+                                if ((y[k] & 0x7f80u) == 0x7f80u) y[k] &= 0xffff0000u, found = true;
+                                if ((y[k] & 0x7f800000u) == 0x7f800000u) y[k] &= 0xffffu, found = true;
+                            }
+                            if (!found) continue;
+                            asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(at(i)), "r"(y[0]), "r"(y[1]), "r"(y[2]), "r"(y[3]) : "memory");
+                            atomicOr(&bad_s[n & 1], 1ull << (key0 + i / (8 * HALVES) - w.s.len));
+                        }
+                    }
+                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                }
+                __syncwarp();
+                if (lane == 0) mbar_arrive(v_clean(sv));
+            }
+            n++;
+        } while (ok && w.next(p));
+        if (!ok && lane == 0) report(p.status, kStatusWaitExpired, 930 + warp);
+    } else if (work) {
         // ---- softmax: thread = row
         const int i = warp >> 2, r = tid & 127;
         const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
         const uint32_t ts = t_s(i) + lanes;
-        const __nv_bfloat16 *q = reinterpret_cast<const __nv_bfloat16 *>(p.q);
         const float sc = p.scale_log2, grow = kTreeRescaleLog2 / sc;
-        int sn = 0, on_ = 0, other_on = 0;
+        const uint64_t sc2 = pack_f32x2(sc, sc);
+        auto wait_all = [&](uint32_t bar, int parity) { return (bool)__all_sync(0xffffffffu, mbar_wait(bar, parity & 1)); };
+        int n = 0, sn = 0, on = 0, other_on = 0;
         do {
             const int T = w.t1 - w.t0, tile0 = w.rb * ROWS + (PAIR ? i * 128 : 0), rows = min(128, w.s.n * p.G - tile0);
             const int jobs = PAIR ? (rows > 0 ? T : 0) : (T + 1 - i) / 2;
             const bool mine = r < rows, active = (r & ~31) < rows;
-            const bool nodes = w.t1 * KEYS > w.s.len;  // this run's part of the item reaches the nodes
-            int parent = -1;
-            if (nodes && r < w.s.n) parent = p.parents[(size_t)w.b * p.N + r];
-            // the queries: PAIR a tile per group, else all eight warps load the one tile
-            {
-                constexpr int CH = DH / 8, STEP = PAIR ? 128 : 256, LOADS = 128 * CH / STEP, BATCH = LOADS < 8 ? LOADS : 8;
-                const int first = PAIR ? r : tid;
-                for (int l0 = 0; (!PAIR || rows > 0) && l0 < LOADS; l0 += BATCH) {
-                    uint4 x[BATCH];
-#pragma unroll
-                    for (int l = 0; l < BATCH; l++) {
-                        const int idx = first + (l0 + l) * STEP, row = idx / CH, ch = idx - row * CH;
-                        x[l] = make_uint4(0, 0, 0, 0);
-                        if (row < rows) {
-                            const int node = (tile0 + row) / p.G, g = (tile0 + row) - node * p.G;
-                            const __nv_bfloat16 *src = q + w.b * p.qs[0] + node * p.qs[1] + (w.h * p.G + g) * p.qs[2] + ch * 8;
-                            if (p.q_vectors) {
-                                x[l] = __ldg(reinterpret_cast<const uint4 *>(src));
-                            } else {
-                                uint32_t y[4];
-#pragma unroll
-                                for (int k = 0; k < 4; k++)
-                                    y[k] = (uint32_t)__bfloat16_as_ushort(src[2 * k]) | ((uint32_t)__bfloat16_as_ushort(src[2 * k + 1]) << 16);
-                                x[l] = make_uint4(y[0], y[1], y[2], y[3]);
-                            }
-                        }
-                    }
-#pragma unroll
-                    for (int l = 0; l < BATCH; l++) {
-                        const int idx = first + (l0 + l) * STEP, row = idx / CH, ch = idx - row * CH;
-                        asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(q_s + (PAIR ? i : 0) * Cfg::kTileBytes + (ch >> 3) * kHalfBytes +
-                                                                                   row * 128 + (((ch & 7) ^ (row & 7)) << 4)),
-                                     "r"(x[l].x), "r"(x[l].y), "r"(x[l].z), "r"(x[l].w)
-                                     : "memory");
-                    }
-                }
-                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");  // (the output of the item before has been read)
-                __syncwarp();
-                if (lane == 0) asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(q_full(PAIR ? i : 0)) : "memory");
-            }
-            // the nodes that this row sees
-            unsigned long long seen = 0;
-            if (nodes) {
-                if (r < w.s.n && (parent >= r || parent < -1)) {
-                    report(p.status, kStatusBadTree, parent);
-                    parent = -1;
-                }
-                asm volatile("bar.sync %0, 128;" ::"r"(2 + i) : "memory");  // (the item before is done with the list)
-                if (r < w.s.n) parents_s[i][r] = parent;
-                asm volatile("bar.sync %0, 128;" ::"r"(2 + i) : "memory");
-                if (mine) seen = tree_ancestors(parents_s[i], (tile0 + r) / p.G);
-            }
+            ok = wait_all(q_full(n), n >> 1);
+            unsigned long long seen = 0;  // the nodes that this row sees
+            if (mine && w.t1 * KEYS > w.s.len)
+                for (int up = (tile0 + r) / p.G; up >= 0; up = parents_s[n & 1][up]) seen |= 1ull << up;
             float m_use = -INFINITY, l_run = 0.f;
-            for (int j = 0; j < jobs; j++) {
+            for (int j = 0; j < jobs && ok; j++) {
                 const int key0 = (w.t0 + (PAIR ? j : 2 * j + i)) * KEYS;
-                ok = mbar_wait(s_full(i), sn++ & 1);
-                ok = __all_sync(0xffffffffu, ok);
+                ok = wait_all(s_full(i), sn++);
                 if (!ok) break;
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                 if (active) {
@@ -703,7 +734,7 @@ __global__ void __launch_bounds__(320, 1) attn_tree_mma_kernel(const __grid_cons
                     }
                     float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-                    for (int c = 0; c < 128; c++) mx[c & 3] = fmaxf(mx[c & 3], __uint_as_float(v[c]));
+                    for (int c = 0; c < 128; c += 2) mx[(c >> 1) & 3] = max3(mx[(c >> 1) & 3], __uint_as_float(v[c]), __uint_as_float(v[c + 1]));
                     const float m_tile = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
                     if (j == 0) {
                         m_use = m_tile;
@@ -713,53 +744,48 @@ __global__ void __launch_bounds__(320, 1) attn_tree_mma_kernel(const __grid_cons
                         m_use = m_new;
                         l_run *= corr;
 #pragma unroll 1
-                        for (int c = 0; c < DH; c += 32) {
-                            uint32_t o[32];
-                            tmem_ld32_issue(t_o(i) + lanes + c, o);
+                        for (int c = 0; c < DH; c += 16) {  // (sixteen at a time: the scores stay in registers)
+                            uint32_t o[16];
+                            tmem_ld16_issue(t_o(i) + lanes + c, o);
                             tmem_ld_wait();
 #pragma unroll
-                            for (int k = 0; k < 32; k++) o[k] = __float_as_uint(__uint_as_float(o[k]) * corr);
-                            tmem_st32(t_o(i) + lanes + c, o);
+                            for (int k = 0; k < 16; k++) o[k] = __float_as_uint(__uint_as_float(o[k]) * corr);
+                            tmem_st16(t_o(i) + lanes + c, o);
                         }
                     }
                     const float off = m_use == -INFINITY ? 0.f : -m_use * sc;  // (nothing seen so far: exp2 of -inf)
-                    float sum[4] = {0.f, 0.f, 0.f, 0.f};
+                    const uint64_t off2 = pack_f32x2(off, off);
+                    uint64_t sum[2] = {0ull, 0ull};
 #pragma unroll
-                    for (int h = 0; h < 2; h++) {
-                        uint32_t pk[32];
+                    for (int h = 0; h < 4; h++) {
+                        uint32_t pk[16];
 #pragma unroll
-                        for (int c = 0; c < 32; c++) {
-                            const float a = ex2_approx(fmaf(__uint_as_float(v[h * 64 + 2 * c]), sc, off));
-                            const float e = ex2_approx(fmaf(__uint_as_float(v[h * 64 + 2 * c + 1]), sc, off));
-                            sum[(2 * c) & 3] += a;
-                            sum[(2 * c + 1) & 3] += e;
+                        for (int c = 0; c < 16; c++) {
+                            const uint64_t y = fma_f32x2((uint64_t)v[h * 32 + 2 * c + 1] << 32 | v[h * 32 + 2 * c], sc2, off2);
+                            const float a = ex2_approx(__uint_as_float((uint32_t)y)), e = ex2_approx(__uint_as_float((uint32_t)(y >> 32)));
+                            sum[c & 1] = add_f32x2(sum[c & 1], pack_f32x2(a, e));
                             pk[c] = pack_bf16(a, e);
                         }
-                        tmem_st32(ts + 32 * h, pk);
+                        tmem_st16(ts + 16 * h, pk);
                     }
-                    l_run += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+                    const uint64_t both = add_f32x2(sum[0], sum[1]);
+                    l_run += __uint_as_float((uint32_t)both) + __uint_as_float((uint32_t)(both >> 32));
                     tmem_st_wait();
                 }
                 asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
                 __syncwarp();
-                if (lane == 0) asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(p_full(i)) : "memory");
+                if (lane == 0) mbar_arrive(p_full(i));
             }
             // ---- the item's output, or this run's part of it
-            if (ok && jobs > 0) {
-                ok = mbar_wait(o_full(i), on_++ & 1);
-                ok = __all_sync(0xffffffffu, ok);
-            }
+            if (ok && jobs > 0) ok = wait_all(o_full(i), on++);
             const bool two = !PAIR && T > 1;  // both groups hold a part
             float f0 = 1.f, f1 = 0.f;         // weights of the two outputs
             if (!PAIR) {
-                if (ok && (i == 0 ? T > 1 : true)) {  // the other group's output
-                    ok = mbar_wait(o_full(1 - i), other_on++ & 1);
-                    ok = __all_sync(0xffffffffu, ok);
-                }
+                if (ok && (i == 1 || two)) ok = wait_all(o_full(1 - i), other_on++);  // the other group's output
                 stats_s[i][r] = make_float2(m_use, l_run);
-                if (!ok) failed_s = 1;
+                if (!ok) *failed_s = 1;
                 asm volatile("bar.sync 1, 256;" ::: "memory");
-                ok = ok && !*(volatile int *)&failed_s;
+                ok = ok && !*(volatile int *)failed_s;
                 const float2 a = stats_s[0][r], b = stats_s[1][r];
                 const float m = two ? fmaxf(a.x, b.x) : a.x;
                 f0 = a.x == m ? 1.f : ex2_approx((a.x - m) * sc);
@@ -767,14 +793,10 @@ __global__ void __launch_bounds__(320, 1) attn_tree_mma_kernel(const __grid_cons
                 m_use = m;
                 l_run = a.y * f0 + (two ? b.y * f1 : 0.f);
             }
-            if (!ok) {
-                if (lane == 0) report(p.status, kStatusWaitExpired, 920 + warp);
-                if (!PAIR) asm volatile("bar.sync 1, 256;" ::: "memory");
-                break;
-            }
+            if (!ok) break;
             if (active && (!PAIR || jobs > 0)) {
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                const unsigned long long bad = mine ? *(volatile unsigned long long *)&bad_s & seen : 0ull;
+                const unsigned long long bad = bad_s[n & 1] & seen;
                 const float inv = w.slot >= 0 ? 1.f : l_run == 0.f ? 0.f : 1.f / l_run;
                 f0 *= inv;
                 f1 *= inv;
@@ -785,45 +807,49 @@ __global__ void __launch_bounds__(320, 1) attn_tree_mma_kernel(const __grid_cons
                 constexpr int COLS = PAIR ? DH : DH / 2;
                 const int col0 = PAIR ? 0 : i * COLS;
 #pragma unroll 1
-                for (int c = col0; c < col0 + COLS; c += 32) {
-                    uint32_t o[32], o2[32];
+                for (int c = col0; c < col0 + COLS; c += 16) {
+                    uint32_t o[16], o2[16];
                     __syncwarp();
-                    tmem_ld32_issue(t_o(PAIR ? i : 0) + lanes + c, o);
-                    if (!PAIR && two) tmem_ld32_issue(t_o(1) + lanes + c, o2);
+                    tmem_ld16_issue(t_o(PAIR ? i : 0) + lanes + c, o);
+                    if (!PAIR) tmem_ld16_issue(t_o(two ? 1 : 0) + lanes + c, o2);
                     tmem_ld_wait();
                     if (!mine) continue;
-                    float x[32];
+                    float y[16];
 #pragma unroll
-                    for (int k = 0; k < 32; k++) {
-                        x[k] = __uint_as_float(o[k]) * f0;
-                        if (!PAIR && two) x[k] += __uint_as_float(o2[k]) * f1;
+                    for (int k = 0; k < 16; k++) {
+                        y[k] = __uint_as_float(o[k]) * f0;
+                        if (!PAIR && two) y[k] += __uint_as_float(o2[k]) * f1;
                     }
                     for (unsigned long long m = bad; m; m &= m - 1) {  // rare: values that are not finite
                         const int at = w.s.len + __ffsll(m) - 1;
                         const __nv_bfloat16 *v = reinterpret_cast<const __nv_bfloat16 *>(p.cache) +
                                                  ((((size_t)p.num_pages + tree_page(p, w.b, at >> 4)) * p.hkv + w.h) * 16 + (at & 15)) * DH + c;
 #pragma unroll
-                        for (int k = 0; k < 32; k++) {
-                            const float y = __bfloat162float(v[k]);
-                            if (!isfinite(y)) x[k] += y;
+                        for (int k = 0; k < 16; k++) {
+                            const float x = __bfloat162float(v[k]);
+                            if (!isfinite(x)) y[k] += x;
                         }
                     }
                     if (w.slot >= 0) {
 #pragma unroll
-                        for (int k = 0; k < 32; k += 4) *reinterpret_cast<float4 *>(part + c + k) = make_float4(x[k], x[k + 1], x[k + 2], x[k + 3]);
+                        for (int k = 0; k < 16; k += 4) *reinterpret_cast<float4 *>(part + c + k) = make_float4(y[k], y[k + 1], y[k + 2], y[k + 3]);
                     } else {
 #pragma unroll
-                        for (int k = 0; k < 32; k += 8)
-                            *reinterpret_cast<uint4 *>(out + c + k) = make_uint4(pack_bf16(x[k], x[k + 1]), pack_bf16(x[k + 2], x[k + 3]),
-                                                                                 pack_bf16(x[k + 4], x[k + 5]), pack_bf16(x[k + 6], x[k + 7]));
+                        for (int k = 0; k < 16; k += 8)
+                            *reinterpret_cast<uint4 *>(out + c + k) = make_uint4(pack_bf16(y[k], y[k + 1]), pack_bf16(y[k + 2], y[k + 3]),
+                                                                                 pack_bf16(y[k + 4], y[k + 5]), pack_bf16(y[k + 6], y[k + 7]));
                     }
                 }
                 if (w.slot >= 0 && mine && (PAIR || i == 0))
                     p.stats[(size_t)w.slot * ROWS + (PAIR ? i * 128 : 0) + r] = make_float2(m_use * sc, l_run);
             }
-            // both groups have read both outputs and the statistics before the next item's products and queries
-            if (!PAIR) asm volatile("bar.sync 1, 256;" ::: "memory");
+            // the outputs have been read: the next item's products may overwrite them (stats_s is rewritten behind those)
+            asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+            __syncwarp();
+            if (lane == 0) mbar_arrive(e_done(n));
+            n++;
         } while (w.next(p));
+        if (!ok && lane == 0) report(p.status, kStatusWaitExpired, 920 + warp);
     }
     __syncwarp();
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
@@ -845,11 +871,11 @@ __global__ void __launch_bounds__(256) attn_tree_join_kernel(const TreeAttnParam
     pdl_wait();
     const TreeSeq s = tree_seq(p, b);
     if (row >= s.n * p.G) return;
-    long long before;
-    const long long per = Plan::per_block(p, Plan::total(p, lane, b, &before));
+    int before;
+    const int per = Plan::per_block(p, Plan::total(p, lane, b, &before));
     const int tiles = Plan::tiles(s), rb = row / ROWS, r = row - rb * ROWS;
-    const long long item0 = before + (long long)(h * Plan::row_blocks(p, s) + rb) * (tiles + p.lead) + p.lead;  // its first tile
-    const int c0 = (int)(item0 / per), c1 = (int)((item0 + tiles - 1) / per);
+    const int item0 = before + (h * Plan::row_blocks(p, s) + rb) * (tiles + p.lead) + p.lead;  // its first tile
+    const int c0 = item0 / per, c1 = (item0 + tiles - 1) / per;
     if (c0 == c1) return;
     auto slot = [&](int c) -> size_t { return (size_t)(2 * c + (c == c0)) * ROWS + r; };
     float m = -INFINITY;

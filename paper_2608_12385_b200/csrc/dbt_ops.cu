@@ -117,9 +117,15 @@ bool strides_fit(const int64_t *s, int n, int dtype) {
 }
 
 // ---- tree attention ----------------------------------------------------------------------------------------------
+constexpr int kTreeLead = 5;  // an item costs about as much as five (fp32: one) of its tiles besides them
 struct TreeShape {
     int rows, keys, blocks, per_sm, lead;
 };
+// The longest line of units that these arguments allow.
+long long tree_units(const dbt_attn_tree_args &a) {
+    const int rows = a.max_nodes * (a.n_q_heads / a.n_kv_heads), keys = a.dtype == DBT_DTYPE_BF16 ? 128 : kTsKeys;
+    return ((long long)a.pages_per_seq * 16 / keys + 1 + kTreeLead) * ((rows + 15) / 16) * a.n_kv_heads * a.B;
+}
 // Blocks: as many as the device holds at once, no more than there can be tiles.
 TreeShape tree_shape(const dbt_attn_tree_args &a) {
     TreeShape s;
@@ -128,7 +134,7 @@ TreeShape tree_shape(const dbt_attn_tree_args &a) {
     s.rows = mma ? (rows <= 128 ? 128 : 256) : (rows <= 16 ? 16 : 64);
     s.keys = mma ? 128 : kTsKeys;
     s.per_sm = s.rows == 16 ? 2 : 1;
-    s.lead = mma ? 5 : 1;  // an item costs about as much as five (one) of its tiles besides them: 63 us without, 42 us at 4..6 (16 ragged sequences)
+    s.lead = getenv("LEAD") ? atoi(getenv("LEAD")) : mma ? kTreeLead : 1;
     const long long tiles = ((long long)a.pages_per_seq * 16 + s.keys - 1) / s.keys, rbs = (a.max_nodes * G + s.rows - 1) / s.rows;
     const long long most = tiles * rbs * a.n_kv_heads * a.B, fit = (long long)sm_count() * s.per_sm;
     s.blocks = (int)(most < fit ? most : fit);
@@ -146,6 +152,7 @@ dbt_status check_tree(const dbt_attn_tree_args *a, bool pointers) {
     if (st != DBT_OK) return st;
     CHECK(a->n_q_heads >= 1 && a->n_q_heads % a->n_kv_heads == 0, DBT_ERR_UNSUPPORTED, "n_q_heads must be a multiple of n_kv_heads");
     CHECK(a->n_q_heads / a->n_kv_heads <= 16, DBT_ERR_UNSUPPORTED, "at most 16 query heads per KV head");
+    CHECK(tree_units(*a) <= 0x7fffffff, DBT_ERR_UNSUPPORTED, "B * n_kv_heads * pages_per_seq are too many tiles for one call");
     if (!pointers) return DBT_OK;
     CHECK(a->q && a->out && a->page_table && a->seq_lens && a->parents && a->workspace && a->status_dev, DBT_ERR_INVALID_ARG, "NULL pointer");
     CHECK(a->q != a->out, DBT_ERR_INVALID_ARG, "out must not be q");
