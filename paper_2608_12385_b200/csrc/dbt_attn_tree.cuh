@@ -27,6 +27,7 @@ struct TreeAttnParams {
     int B, N, G, hkv, num_pages, pps, blocks;
     int lead;       // empty units ahead of an item
     int q_vectors;  // queries can be read in 16-byte vectors
+    int g_inverse;  // 2^16 / G rounded up: (row * g_inverse) >> 16 is row / G up to 1024 rows
     float scale_log2;  // softmax scale * log2(e)
 };
 
@@ -605,36 +606,28 @@ __global__ void __launch_bounds__(384, 1) attn_tree_mma_kernel(const __grid_cons
             if (n > 1) ok = wait(e_done(n - 2), (n - 2) >> 1);  // the buffers of the item before the last are free
             if (ok && n > 0) ok = wait(q_empty, n - 1);
             if (!ok) break;
-            constexpr int CH = DH / 8, LOADS = Cfg::kQTiles * 128 * CH / 64, BATCH = 4;
-            for (int l0 = 0; l0 < LOADS; l0 += BATCH) {
-                uint4 v[BATCH];
+            // 64 threads are few: all their copies are under way at once (through registers, a few at a time, the first queries of
+            // a block took 14 us of 64 KB)
+            constexpr int CH = DH / 8, LOADS = Cfg::kQTiles * 128 * CH / 64, STEP = 64 / CH;
+            const int ch = x % CH;
+            const __nv_bfloat16 *base = q + w.b * p.qs[0] + w.h * p.G * p.qs[2] + ch * 8;
+#pragma unroll 4
+            for (int l = 0; l < LOADS; l++) {
+                const int row = x / CH + l * STEP, node = ((row0 + row) * p.g_inverse) >> 16, g = row0 + row - node * p.G;
+                const uint32_t dst = q_s + (row >> 7) * Cfg::kTileBytes + (ch >> 3) * kHalfBytes + (row & 127) * 128 + (((ch & 7) ^ (row & 7)) << 4);
+                const __nv_bfloat16 *src = row < rows ? base + node * p.qs[1] + g * p.qs[2] : q;
+                if (p.q_vectors) {
+                    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(row < rows ? 16 : 0) : "memory");
+                } else {
+                    uint32_t y[4] = {0, 0, 0, 0};
+                    if (row < rows)
 #pragma unroll
-                for (int l = 0; l < BATCH; l++) {
-                    const int idx = x + (l0 + l) * 64, row = idx / CH, ch = idx - row * CH;
-                    v[l] = make_uint4(0, 0, 0, 0);
-                    if (row < rows) {
-                        const int node = (row0 + row) / p.G, g = (row0 + row) - node * p.G;
-                        const __nv_bfloat16 *src = q + w.b * p.qs[0] + node * p.qs[1] + (w.h * p.G + g) * p.qs[2] + ch * 8;
-                        if (p.q_vectors) {
-                            v[l] = __ldg(reinterpret_cast<const uint4 *>(src));
-                        } else {
-                            uint32_t y[4];
-#pragma unroll
-                            for (int k = 0; k < 4; k++)
-                                y[k] = (uint32_t)__bfloat16_as_ushort(src[2 * k]) | ((uint32_t)__bfloat16_as_ushort(src[2 * k + 1]) << 16);
-                            v[l] = make_uint4(y[0], y[1], y[2], y[3]);
-                        }
-                    }
-                }
-#pragma unroll
-                for (int l = 0; l < BATCH; l++) {
-                    const int idx = x + (l0 + l) * 64, row = idx / CH, ch = idx - row * CH;
-                    asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(q_s + (row >> 7) * Cfg::kTileBytes + (ch >> 3) * kHalfBytes +
-                                                                               (row & 127) * 128 + (((ch & 7) ^ (row & 7)) << 4)),
-                                 "r"(v[l].x), "r"(v[l].y), "r"(v[l].z), "r"(v[l].w)
-                                 : "memory");
+                        for (int k = 0; k < 4; k++)
+                            y[k] = (uint32_t)__bfloat16_as_ushort(src[2 * k]) | ((uint32_t)__bfloat16_as_ushort(src[2 * k + 1]) << 16);
+                    asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(dst), "r"(y[0]), "r"(y[1]), "r"(y[2]), "r"(y[3]) : "memory");
                 }
             }
+            asm volatile("cp.async.wait_all;" ::: "memory");
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
             // a bad parent counts as none
             if (x < w.s.n && (parent >= x || parent < -1)) report(p.status, kStatusBadTree, parent);

@@ -344,6 +344,7 @@ dbt_status dbt_op_attn_tree(const dbt_attn_tree_args *a, void *cuda_stream) {
     p.pps = a->pages_per_seq;
     p.blocks = s.blocks;
     p.lead = s.lead;
+    p.g_inverse = (65536 + p.G - 1) / p.G;
     p.q_vectors = aligned(a->q, 16) && strides_fit(a->q_stride, 3, a->dtype);
     p.scale_log2 = (a->softmax_scale > 0.f ? a->softmax_scale : 1.f / std::sqrt((float)a->head_dim)) * 1.4426950408889634f;
     cudaError_t e;
