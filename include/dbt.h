@@ -173,6 +173,21 @@ dbt_status dbt_decode_step(dbt_model *m, const int32_t *tokens_dev, int32_t B, i
 dbt_status dbt_decode_step_primary_only(dbt_model *m, const int32_t *tokens_dev, int32_t B,
                                         int32_t *next_tokens_dev, float *logits_primary_dev);
 
+/* Tokens drawn from the last step's output distribution instead of its argmax: for the sequences 0..B-1 of the last
+ * dbt_decode_step, dbt_decode_step_primary_only or dbt_prefill_boundary of this handle (their *_host forms too), by the rules
+ * of dbt_op_sample below with z = log(alpha p + (1 - alpha) q), the mixture of Eq. mixloss and Appendix C.1 (primary-only
+ * steps: the primary logits), so that the temperature acts on the mixture.  s HOST, its entries DEVICE [B], all but uniforms may
+ * be NULL.  next_tokens_dev int32 [B], logprobs_dev fp32 [B] or NULL.  May be called again for other numbers.
+ * DBT_ERR_STATE: no step yet, or a dbt_prefill or dbt_reset since.  DBT_ERR_INVALID_ARG: B is not the last step's. */
+typedef struct {
+    uint32_t struct_size; /* sizeof(dbt_sampling) */
+    int32_t reserved;     /* 0 */
+    const float *uniforms, *temperature;
+    const int32_t *top_k;
+    const float *top_p, *min_p;
+} dbt_sampling;
+dbt_status dbt_sample_last(dbt_model *m, const dbt_sampling *s, int32_t B, int32_t *next_tokens_dev, float *logprobs_dev);
+
 /* End-to-end variants with HOST buffers: copy tokens_host [B] to the device, run the step,
  * copy next_tokens_host [B] (and alpha_host [B] when non-NULL) back, wait for the stream.
  * Buffers should be pinned for the copies to be asynchronous. */

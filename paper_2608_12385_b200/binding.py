@@ -29,7 +29,7 @@ EXPORTS = ["dbt_query_sizes", "dbt_create", "dbt_destroy", "dbt_set_page_table",
            "dbt_launch_count", "dbt_last_error", "dbt_version", "dbt_profile_begin", "dbt_profile_end", "dbt_op_gemm_tc",
            "dbt_op_gemm_tc_static", "dbt_kv_export", "dbt_kv_import", "dbt_prefill_boundary", "dbt_rope_frequencies",
            "dbt_op_rope", "dbt_op_rope_append", "dbt_op_attn_tree_workspace", "dbt_op_attn_tree", "dbt_op_sample",
-           "dbt_op_tree_accept"]
+           "dbt_op_tree_accept", "dbt_sample_last"]
 
 
 class DbtError(RuntimeError):
@@ -108,6 +108,7 @@ def load_library():
     L.dbt_op_attn_tree.argtypes = [vp, vp]
     L.dbt_op_sample.argtypes = [vp, i32, i32, i32, C.c_int64, vp, vp, vp, vp, vp, vp, vp, vp]
     L.dbt_op_tree_accept.argtypes = [vp, vp]
+    L.dbt_sample_last.argtypes = [vp, vp, i32, vp, vp]
     L.dbt_profile_begin.argtypes = [vp]
     L.dbt_profile_end.argtypes = [vp, C.POINTER(DbtProfileEntry), i32, i32p]
     L.dbt_launch_count.argtypes = [vp]
@@ -199,6 +200,7 @@ ROPE_SPEC_FORMAT = struct.Struct("@I3i5d")
 ROPE_APPEND_FORMAT = struct.Struct("@I10if3P9q2P4PPP")
 ATTN_TREE_FORMAT = struct.Struct("@I8if2P3qP4PPNP")
 TREE_ACCEPT_FORMAT = struct.Struct("@I8i6PP4PP")
+SAMPLING_FORMAT = struct.Struct("@Ii5P")
 ROPE_KINDS = {"plain": 0, "linear": 1, "base": 2, "ramp": 3, "bands": 4}
 _DTYPES = {torch.float32: 0, torch.bfloat16: 1}
 
@@ -585,6 +587,21 @@ class Model:
     def decode_step_primary_only(self, tokens_dev: torch.Tensor, next_dev: torch.Tensor | None = None, z1=None):
         B = tokens_dev.shape[0]
         self._check(self.L.dbt_decode_step_primary_only(self._h, tokens_dev.data_ptr(), B, _p(next_dev), _p(z1)))
+
+    def sample_last(self, uniforms: torch.Tensor, temperature: torch.Tensor | None = None, top_k: torch.Tensor | None = None,
+                    top_p: torch.Tensor | None = None, min_p: torch.Tensor | None = None, next_dev: torch.Tensor | None = None):
+        """Tokens of the last step (any of the step calls, or prefill_boundary) drawn from its mixture by the rules of op_sample instead of
+        picked: (tokens int32 [B], log of each token's share).  The tensors have to be ready on the model's stream."""
+        B = uniforms.shape[0]
+        if next_dev is None:
+            next_dev = torch.empty(B, dtype=torch.int32, device=self.device)
+        logprobs = torch.empty(B, dtype=torch.float32, device=self.device)
+        _refuse(uniforms=(uniforms, _F32, (B,)), temperature=(temperature, _F32, (B,)), top_k=(top_k, _I32, (B,)), top_p=(top_p, _F32, (B,)),
+                min_p=(min_p, _F32, (B,)), next_dev=(next_dev, _I32, (B,)))
+        _stream(self.device.index, (uniforms, temperature, top_k, top_p, min_p, next_dev))
+        self._check(self.L.dbt_sample_last(self._h, SAMPLING_FORMAT.pack(SAMPLING_FORMAT.size, 0, uniforms.data_ptr(), _p(temperature) or 0, _p(top_k) or 0,
+                                                                         _p(top_p) or 0, _p(min_p) or 0), B, next_dev.data_ptr(), logprobs.data_ptr()))
+        return next_dev, logprobs
 
     def decode_step_host(self, tokens_host: torch.Tensor, next_host: torch.Tensor, alpha_host=None):
         self._check(self.L.dbt_decode_step_host(self._h, tokens_host.data_ptr(), tokens_host.shape[0],

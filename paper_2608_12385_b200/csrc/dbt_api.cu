@@ -50,6 +50,7 @@ struct Workspace {
     // MoE on tensor cores: activation rows sorted by expert
     __nv_bfloat16 *Xs, *Hs;
     float *Pe;
+    float *scores;        // dbt_sample_last: what tokens are drawn by, [max_batch][V]
     float *ro_stats;      // readout: per (sequence, vocabulary chunk) softmax records and argmax candidates
     int32_t *ro_tickets;  // readout: arrival counters per sequence
     float *P2;       // split-K partials of the shared expert's GEMMs when they run beside the routed chain
@@ -85,6 +86,7 @@ struct dbt_model {
     int64_t launches;
     std::string err;
     bool pending_union;
+    int last_B, last_grouped;  // the step whose logits stand in the workspace (last_B = 0: none)
     // optional per-launch timing (dbt_profile_begin / dbt_profile_end)
     bool prof_on;
     struct ProfRec { const char *tag; double bytes; cudaEvent_t e0, e1; };
@@ -267,6 +269,7 @@ size_t carve(const dbt_config &c, char *base, Workspace *ws, int *Rmax_out, int 
     w.att_tickets = k.take<int32_t>((size_t)att_rows * c.n_kv_heads);
     w.att_tickets2 = k.take<int32_t>((size_t)att_rows * c.n_kv_heads * kAttMaxGroups);
     w.ro_stats = k.take<float>((size_t)c.max_batch * kRoMaxChunks * kRoRec);
+    w.scores = k.take<float>((size_t)c.max_batch * c.vocab);
     w.ro_tickets = k.take<int32_t>(c.max_batch);
     w.gemm_tickets = k.take<int32_t>(4096);
     w.tokens_stage = k.take<int32_t>(c.max_batch);
@@ -2553,6 +2556,7 @@ dbt_status dbt_reset(dbt_model *m) {
     CUDA_TRY(m, cudaMemsetAsync(m->ws.gemm_tickets, 0, sizeof(int32_t) * 4096, m->stream));
     CUDA_TRY(m, cudaMemsetAsync(m->ws.ro_tickets, 0, sizeof(int32_t) * (size_t)m->cfg.max_batch, m->stream));
     std::fill(m->len_host.begin(), m->len_host.end(), 0);
+    m->last_B = 0;
     return DBT_OK;
 }
 
@@ -2577,6 +2581,7 @@ int32_t dbt_seq_len(const dbt_model *m, int32_t b) {
 dbt_status dbt_prefill(dbt_model *m, const int32_t *tokens_dev, int32_t B, int32_t n, float *last_primary_logits_dev) {
     dbt_status st = check_step_args(m, tokens_dev, B, n);
     if (st != DBT_OK) return st;
+    m->last_B = 0;  // (a chunk's logits take the place of the last step's)
     if (m->cfg.weight_dtype == DBT_DTYPE_F32) return prefill_impl<float>(m, tokens_dev, B, n, last_primary_logits_dev);
     if (m->wide) return prefill_wide(m, tokens_dev, B, n, last_primary_logits_dev, false);
     if (m->tc) return prefill_tc(m, tokens_dev, B, n, last_primary_logits_dev, false);
@@ -2644,17 +2649,26 @@ static dbt_status step_graphed(dbt_model *m, const int32_t *tokens_dev, int B, i
     return DBT_OK;
 }
 
+// Remember whose logits stand in the workspace.
+static dbt_status step_done(dbt_model *m, int B, int grouped, dbt_status st) {
+    m->last_B = st == DBT_OK ? B : 0;
+    m->last_grouped = grouped;
+    return st;
+}
+
 dbt_status dbt_decode_step(dbt_model *m, const int32_t *tokens_dev, int32_t B, int32_t *next_tokens_dev,
                            float *logits_primary_dev, float *logits_branch_dev, float *alpha_dev) {
     dbt_status st = check_step_args(m, tokens_dev, B, 1);
     if (st != DBT_OK || (st = check_step_rows(m, B, paths_of(m->cfg))) != DBT_OK) return st;
-    return step_graphed(m, tokens_dev, B, paths_of(m->cfg), next_tokens_dev, logits_primary_dev, logits_branch_dev, alpha_dev);
+    return step_done(m, B, paths_of(m->cfg),
+                     step_graphed(m, tokens_dev, B, paths_of(m->cfg), next_tokens_dev, logits_primary_dev, logits_branch_dev, alpha_dev));
 }
 
 dbt_status dbt_prefill_boundary(dbt_model *m, const int32_t *tokens_dev, int32_t B, int32_t S, int32_t *next_tokens_dev,
                                 float *logits_primary_dev, float *logits_branch_dev, float *alpha_dev) {
     dbt_status st = check_step_args(m, tokens_dev, B, S);
     if (st != DBT_OK || (st = check_step_rows(m, B, paths_of(m->cfg))) != DBT_OK) return st;
+    m->last_B = 0;
     if (S > 1) {
         // positions 1..S-1 of every row of tokens_dev [B][S]: the prompt-wide prefill walks rows of stride S
         m->tok_stride = S;
@@ -2677,14 +2691,37 @@ dbt_status dbt_prefill_boundary(dbt_model *m, const int32_t *tokens_dev, int32_t
     m->tok_p0 = 0;
     m->step_l0 = 0;
     m->ride = RideRows{};
-    return st;
+    return step_done(m, B, paths_of(m->cfg), st);
+}
+
+dbt_status dbt_sample_last(dbt_model *m, const dbt_sampling *s, int32_t B, int32_t *next_tokens_dev, float *logprobs_dev) {
+    if (!m) return DBT_ERR_INVALID_ARG;
+    if (!s || s->struct_size != sizeof(dbt_sampling)) return fail(m, DBT_ERR_INVALID_ARG, "dbt_sampling: NULL, or another struct_size");
+    if (!s->uniforms || !next_tokens_dev) return fail(m, DBT_ERR_INVALID_ARG, "NULL pointer");
+    if (m->last_B == 0) return fail(m, DBT_ERR_STATE, "no step's logits to sample from");
+    const dbt_config &c = m->cfg;
+    const Workspace &w = m->ws;
+    if (B != m->last_B) return fail(m, DBT_ERR_INVALID_ARG, "the last step had %d sequences (B=%d)", m->last_B, B);
+    const int P = m->last_grouped, nc = (c.vocab + kRoChunk - 1) / kRoChunk, chunk = (c.vocab + nc - 1) / nc;
+    if (nc > kRoMaxChunks) return fail(m, DBT_ERR_UNSUPPORTED, "at most %d tokens in the vocabulary", kRoChunk * kRoMaxChunks);
+    const float *scores = w.Z;  // primary-only steps: the logits themselves
+    if (P > 1) {
+        LAUNCH(m, "readout_stats", 0, readout_stats_kernel, dim3(B, nc), kRoThreads, 0, w.Z, B, c.vocab, P, chunk, w.ro_stats);
+        LAUNCH(m, "mix_scores", 0, mix_scores_kernel, dim3(B, nc), kRoThreads, 0, w.Z, B, c.vocab, chunk, P, w.ro_stats, w.scores);
+        scores = w.scores;
+    }
+    dbt_status st = dbt_op_sample(scores, DBT_DTYPE_F32, B, c.vocab, c.vocab, s->uniforms, s->temperature, s->top_k, s->top_p, s->min_p,
+                                  next_tokens_dev, logprobs_dev, m->stream);
+    if (st != DBT_OK) return fail(m, st, "%s", g_create_error.c_str());
+    m->launches++;
+    return DBT_OK;
 }
 
 dbt_status dbt_decode_step_primary_only(dbt_model *m, const int32_t *tokens_dev, int32_t B, int32_t *next_tokens_dev,
                                         float *logits_primary_dev) {
     dbt_status st = check_step_args(m, tokens_dev, B, 1);
     if (st != DBT_OK || (st = check_step_rows(m, B, 0)) != DBT_OK) return st;
-    return step_graphed(m, tokens_dev, B, 0, next_tokens_dev, logits_primary_dev, nullptr, nullptr);
+    return step_done(m, B, 0, step_graphed(m, tokens_dev, B, 0, next_tokens_dev, logits_primary_dev, nullptr, nullptr));
 }
 
 static dbt_status step_host(dbt_model *m, const int32_t *tokens_host, int32_t B, int32_t *next_host, float *alpha_host,

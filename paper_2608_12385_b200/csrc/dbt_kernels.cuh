@@ -877,6 +877,44 @@ __global__ void moe_lists_kernel(const int32_t *idx, int R, int kmax, int E, int
     if (c > 0 && union_count) atomicAdd(union_count, 1);
 }
 
+// Scores that the tokens of a step are drawn by: log(alpha p + (1 - alpha) mean_j q_j) (Eq. alpha, Eq. mixloss; Appendix C.1) from the
+// records of readout_stats_kernel, a CTA per (row, chunk).  A sampler's temperature then acts on the mixture itself.
+__global__ void __launch_bounds__(kRoThreads) mix_scores_kernel(const float *Z, int B, int V, int chunk, int P, const float *stats, float *scores) {
+    pdl_enter();
+    __shared__ float glob[3 + 2 * kMaxBranches];  // m1, d1, alpha, then (m_j, d_j) per branch
+    const int b = blockIdx.x, ck = blockIdx.y, nc = gridDim.y, tid = threadIdx.x, lane = tid & 31;
+    const int v0 = ck * chunk, v1 = min(V, v0 + chunk), nb = P - 1;
+    if (tid < 32) {
+        const float *rec = stats + (size_t)b * nc * kRoRec;
+        for (int j = 0; j <= nb; j++) {
+            const int at = j == 0 ? 0 : 3 + 2 * j;
+            float m = -INFINITY, s = 0.f, sq = 0.f;
+            for (int k = lane; k < nc; k += 32) m = fmaxf(m, __ldcg(rec + (size_t)k * kRoRec + at));
+            m = warp_max(m);
+            for (int k = lane; k < nc; k += 32) {
+                const float f = expf(__ldcg(rec + (size_t)k * kRoRec + at) - m);
+                s += __ldcg(rec + (size_t)k * kRoRec + at + 1) * f;
+                if (j == 0) sq += __ldcg(rec + (size_t)k * kRoRec + 2) * f * f;
+            }
+            s = warp_sum(s);
+            sq = warp_sum(sq);
+            if (lane == 0) {
+                const int to = j == 0 ? 0 : 1 + 2 * j;
+                glob[to] = m;
+                glob[to + 1] = s;
+                if (j == 0) glob[2] = fminf(1.f, fmaxf(0.5f, sq / (s * s)));
+            }
+        }
+    }
+    __syncthreads();
+    const float m1 = glob[0], d1 = glob[1], alpha = glob[2], inv_nb = 1.f / (float)nb;
+    for (int v = v0 + tid; v < v1; v += kRoThreads) {
+        float q = 0.f;
+        for (int j = 0; j < nb; j++) q += expf(__ldcg(Z + (size_t)((j + 1) * B + b) * V + v) - glob[3 + 2 * j]) / glob[4 + 2 * j];
+        scores[(size_t)b * V + v] = logf(alpha * (expf(__ldcg(Z + (size_t)b * V + v) - m1) / d1) + (1.f - alpha) * (q * inv_nb));
+    }
+}
+
 // Routed experts, gate/up + SwiGLU: every expert with a non-empty list streams its gate and up
 // matrices once for all its entries of both paths.  grid (ceil(Fe/warps), E).
 template <typename WT>

@@ -119,7 +119,9 @@ bool strides_fit(const int64_t *s, int n, int dtype) {
 }
 
 // ---- tree attention ----------------------------------------------------------------------------------------------
-constexpr int kTreeLead = 5;  // an item costs about as much as five (fp32: one) of its tiles besides them
+// An item costs about as much as five (fp32: one) of its tiles besides them: 16 ragged sequences 63 us without, 42 us with four to six
+// (then), 37, 36, 39 us with three, five, eight (now); long items do not care.
+constexpr int kTreeLead = 5;
 struct TreeShape {
     int rows, keys, blocks, per_sm, lead;
 };
@@ -136,7 +138,7 @@ TreeShape tree_shape(const dbt_attn_tree_args &a) {
     s.rows = mma ? (rows <= 128 ? 128 : 256) : (rows <= 16 ? 16 : 64);
     s.keys = mma ? 128 : kTsKeys;
     s.per_sm = s.rows == 16 ? 2 : 1;
-    s.lead = getenv("LEAD") ? atoi(getenv("LEAD")) : mma ? kTreeLead : 1;
+    s.lead = mma ? kTreeLead : 1;
     const long long tiles = ((long long)a.pages_per_seq * 16 + s.keys - 1) / s.keys, rbs = (a.max_nodes * G + s.rows - 1) / s.rows;
     const long long most = tiles * rbs * a.n_kv_heads * a.B, fit = (long long)sm_count() * s.per_sm;
     s.blocks = (int)(most < fit ? most : fit);

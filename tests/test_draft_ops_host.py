@@ -22,6 +22,7 @@ def lib():
 
 
 STRUCTS = {
+    "dbt_sampling": (binding.SAMPLING_FORMAT, "reserved uniforms temperature top_k top_p min_p"),
     "dbt_rope_spec": (binding.ROPE_SPEC_FORMAT, "kind rot_dim reserved base factor trained_len low high"),
     "dbt_rope_append_args": (binding.ROPE_APPEND_FORMAT,
                              "dtype B max_nodes n_q_heads n_kv_heads head_dim rot_dim interleaved num_pages pages_per_seq scale q k v q_stride[0] "
@@ -57,7 +58,7 @@ def test_argument_formats_have_the_headers_layout(name):
 
 
 POINTERS = set("q k v q_out cache_layer positions page_table seq_lens node_counts freq status_dev out parents workspace tokens sampled pool path "
-               "counts next_tokens new_lens".split())
+               "counts next_tokens new_lens uniforms temperature top_k top_p min_p".split())
 
 
 def refused(lib, st, code, text=""):
@@ -139,6 +140,10 @@ def test_sample_refusals(lib, change, code, text):
     a = dict(logits=PTR, dtype=0, rows=2, vocab=100, stride=100, u=PTR, t=0, k=0, p=0, m=0, tokens=PTR, logprobs=0)
     a.update(change)
     refused(lib, lib.dbt_op_sample(*a.values(), None), code, text)
+
+
+def test_sample_last_needs_a_handle(lib):
+    assert lib.dbt_sample_last(None, None, 1, None, None) == 1
 
 
 def test_sample_of_no_rows_is_nothing(lib):

@@ -1,0 +1,134 @@
+"""Tokens drawn from a step's mixture (dbt_sample_last) against the 64-bit forms of the mixture and of the sampler, on the
+logits and alpha that the same step hands out."""
+import numpy as np
+import pytest
+import torch
+
+import ref_drafts as ref
+from gpu_util import library
+from paper_2608_12385_b200 import binding
+from paper_2608_12385_b200.inputs import ModelConfig, make_tokens, make_weights
+
+pytestmark = pytest.mark.gpu
+
+DENSE = ModelConfig(d_model=256, n_layers=2, n_q_heads=4, n_kv_heads=2, head_dim=64, d_ff=704, vocab=5000, weight_dtype="bf16")
+CONFIGS = {
+    "bf16": DENSE,
+    "bf16-4-paths": DENSE.replace(n_paths=4),
+    "fp32": DENSE.replace(weight_dtype="fp32", vocab=900),
+    "moe": DENSE.replace(n_experts=8, d_expert=128, n_shared_experts=1, k_primary=2, k_branch=2, d_ff=0),
+}
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _lib():
+    library()
+
+
+def model(cfg, B):
+    return binding.Model(cfg, binding.weights_to_device(make_weights(cfg, seed=0, matrix_std=0.08), "cuda:0"), B, 64)
+
+
+def mixture_scores(out):
+    z1, z2, alpha = (out[k].double().cpu() for k in ("z1", "z2", "alpha"))
+    q = torch.softmax(z2, dim=-1)
+    return torch.log(alpha[:, None] * torch.softmax(z1, dim=-1) + (1 - alpha[:, None]) * (q.mean(0) if q.dim() == 3 else q)).numpy()
+
+
+def check(scores, drawn, u, kw, B):
+    """Scores are fp32 logarithms of sums of exponentials and quotients of fp32: off by at most 2^-18 where they are above -80 (an
+    exponential's argument of at most 80 in fp32 is off by 2^-18, the rest is below that).  A running sum moves by no more, relative; a
+    token has to be the 64-bit form's unless a decision is closer than that."""
+    tok, lp = drawn[0].cpu().tolist(), drawn[1].cpu().tolist()
+    sure = 0
+    for b in range(B):
+        at = lambda k, d: d if k not in kw else float(kw[k][b])  # noqa: E731
+        want, logp, near = ref.sample_row(scores[b], float(np.float32(u[b])), at("temperature", 1.0), int(at("top_k", 0)), at("top_p", 1.0), at("min_p", 0.0))
+        t = at("temperature", 1.0)
+        if near < 2.0 ** -16 / max(min(t, 1.0), 0.1):
+            continue
+        if at("top_k", 0) > 0:  # the border of top-k: two scores closer than their error may change places
+            z = np.sort(scores[b])[::-1]
+            if z[int(at("top_k", 0)) - 1] - z[int(at("top_k", 0))] < 2.0 ** -16:
+                continue
+        sure += 1
+        assert tok[b] == want, (b, tok[b], want, near)
+        assert abs(lp[b] - logp) <= 2.0 ** -14 / max(min(t, 1.0), 0.1)
+    return sure
+
+
+@pytest.mark.parametrize("name", sorted(CONFIGS))
+def test_sampling_from_the_mixture(name):
+    cfg, B = CONFIGS[name], 4
+    m = model(cfg, B)
+    tok = make_tokens(cfg, B, 12, seed=1).cuda()
+    m.prefill(tok[:, :8].contiguous())
+    g = torch.Generator().manual_seed(5)
+    sure = 0
+    for t in range(8, 12):
+        out = m.decode_full(tok[:, t].contiguous())
+        scores = mixture_scores(out)
+        for kw in ({}, dict(temperature=[0.7] * B), dict(top_k=[5, 40, 0, 300], top_p=[0.9] * B), dict(min_p=[0.05] * B, temperature=[1.3] * B)):
+            u = torch.rand(B, generator=g)
+            dev = {k: torch.tensor(v, dtype=torch.int32 if k == "top_k" else torch.float32).cuda() for k, v in kw.items()}
+            sure += check(scores, m.sample_last(u.cuda(), **dev), u.tolist(), kw, B)
+        greedy = m.sample_last(torch.zeros(B, device="cuda"), temperature=torch.zeros(B, device="cuda"))[0]
+        gap = np.sort(scores, axis=1)[:, ::-1]
+        for b in range(B):
+            if gap[b, 0] - gap[b, 1] > 2.0 ** -16:
+                assert int(greedy[b]) == int(out["next"][b])
+    assert sure >= 40  # most draws are decided
+    assert m.sync_status() == (0, 0)
+
+
+def test_sampling_after_primary_only_and_boundary_steps():
+    cfg, B = CONFIGS["bf16"], 3
+    m = model(cfg, B)
+    tok = make_tokens(cfg, B, 10, seed=2).cuda()
+    u = torch.rand(B, generator=torch.Generator().manual_seed(6))
+    out = m.prefill_boundary(tok[:, :9].contiguous())
+    assert check(mixture_scores(out), m.sample_last(u.cuda()), u.tolist(), {}, B) >= 1
+    out = m.decode_full(tok[:, 9].contiguous(), grouped=False)
+    drawn = m.sample_last(u.cuda(), top_k=torch.full((B,), 20, dtype=torch.int32, device="cuda"))
+    want = [ref.sample_row(out["z1"][b].cpu().numpy(), float(u[b]), top_k=20) for b in range(B)]
+    assert drawn[0].tolist() == [w[0] for w in want]  # the logits themselves: exact
+
+
+def test_sampled_decoding_feeds_itself_and_leaves_the_cache_as_greedy_steps_do():
+    """The drawn token written straight into the next step's input; the cache holds what teacher-forced steps write."""
+    cfg, B = CONFIGS["bf16"], 2
+    m, n = model(cfg, B), model(cfg, B)
+    tok = make_tokens(cfg, B, 5, seed=3).cuda()
+    for x in (m, n):
+        x.prefill(tok[:, :4].contiguous())
+    cur, g, fed = tok[:, 4].contiguous(), torch.Generator().manual_seed(7), []
+    for _ in range(10):
+        fed.append(cur.clone())
+        m.decode_step(cur)
+        m.sample_last(torch.rand(B, generator=g).cuda(), top_p=torch.full((B,), 0.9, device="cuda"), next_dev=cur)
+    for t in fed:
+        n.decode_step(t.clone())
+    for a, b in zip(m.export_kv(B, 14), n.export_kv(B, 14)):
+        assert torch.equal(a, b)
+    assert len({int(t[0]) for t in fed}) > 3
+
+
+def test_refusals():
+    cfg, B = CONFIGS["fp32"], 2
+    m = model(cfg, B)
+    tok, u = make_tokens(cfg, B, 4, seed=4).cuda(), torch.zeros(B, device="cuda")
+    for prepare, status in ((lambda: None, 4), (lambda: m.prefill(tok[:, :3].contiguous()), 4)):
+        prepare()
+        with pytest.raises(binding.DbtError) as e:
+            m.sample_last(u)
+        assert e.value.status == status
+    m.decode_full(tok[:, 3].contiguous())
+    m.sample_last(u)
+    for bad in (lambda: m.sample_last(torch.zeros(1, device="cuda")), lambda: m.sample_last(u, top_k=u), lambda: m.sample_last(u.cpu())):
+        with pytest.raises(binding.DbtError) as e:
+            bad()
+        assert e.value.status == 1
+    m.reset()
+    with pytest.raises(binding.DbtError) as e:
+        m.sample_last(u)
+    assert e.value.status == 4
