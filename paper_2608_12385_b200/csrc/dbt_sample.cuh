@@ -12,11 +12,17 @@
 // largest of these maxima has at least K values of the row at or above it, and seldom many more.  What lies above that bound (K = top_k, or 512 where top-p alone asks)
 // is sent to the first block, which sorts it and finishes alone, if the kept set turns out to lie inside.
 //
-// The long way, for flat rows, ties and large top_k.  The border of a filter is found by narrowing: the row's values between
+// The middle way, where more is kept.  The values' counts in 1024 equal steps below the largest (taken along in a pass that is made
+// anyway) say in which steps the border must lie -- by count exactly, by mass up to what the steps' width leaves open --; one pass
+// forms the mass above them and sends what lies in them to the first block, which sorts it and finds the border, exactly or
+// not at all.
+//
+// The long way, for ties and whatever the others leave.  The border of a filter is found by narrowing: the row's values between
 // two bounds are dropped into 16 buckets (equal steps of the float's ordered bit pattern, the last one open below), the blocks
 // add up their counts and masses, and the bucket that holds the border is the next range, until what lies above the range and
-// in it, or at least the range itself, is a list that one block can sort, or a single value.  Where the kept set is larger than a
-// list, a pass in the order of ids sums what is kept, 256 ids at a time.
+// in it, or at least the range itself, is a list that one block can sort, or a single value.
+//
+// Where the kept set is larger than a list, a pass in the order of ids sums what is kept, 256 ids at a time.
 //
 // Masses are 64-bit sums of 64-bit exponentials: which id a number falls on hangs on the last bits of sums over the
 // vocabulary; with 128256 tokens fp32 would move the border of one row in a few hundred.  The exponential is table-driven (16
@@ -40,6 +46,7 @@ constexpr int kSmList = 1024;    // values that one block sorts
 constexpr int kSmGuess = 512;    // values that the short way asks for where top-k does not say, and its largest top_k
 constexpr int kSmMaxBuckets = 64;  // for the threads' maxima
 constexpr int kSmRun = 256;      // ids summed together by a warp on the long way
+constexpr int kSmSteps = 1024;   // of the middle way
 constexpr int kSmMaxCluster = 8;
 constexpr int kSmMaxSlice = 32768;  // values of a row per block
 // Scratch area: the list's keys, w and sums, or bucket masses per thread.
@@ -73,6 +80,7 @@ struct SampleShared {
     int warp_i[32];
     int counts[kSmBuckets];
     int found, sent;
+    unsigned slots;  // list entries handed out to the cluster (first block)
     union {
         struct {
             int local[kSmMaxBuckets], all[kSmMaxCluster][kSmMaxBuckets];  // short way: the threads' maxima by bucket
@@ -683,6 +691,7 @@ __global__ void __launch_bounds__(NT, NT == 256 ? 4 : 1) sample_kernel(const Sam
         sh.local[0] = mx;
         sh.local[1] = low_max;
         sh.sent = 0;
+        sh.slots = 0;
     }
     if (tid < kSmMaxBuckets) sh.maxima.local[tid] = 0;
     {
@@ -728,6 +737,16 @@ __global__ void __launch_bounds__(NT, NT == 256 ? 4 : 1) sample_kernel(const Sam
         double total;
         SampleRange range;
     } known{};
+    // ---- the middle way's steps: this block's counts, and the cluster's in the first block, behind the list's first two places
+    int *steps = reinterpret_cast<int *>(row.scratch + 2 * kSmList), *all_steps = steps + kSmSteps;
+    static_assert(2 * kSmSteps * 4 <= kSmList * 8, "the counts fit the list's third place");
+    const float per_step = kSmSteps / (f.k_on ? fmaxf(mx - low_max, 1e-30f) : 16.f * temp);  // (by mass 16 T: e^-16 of the largest)
+    auto step_of = [&](float z) { return (int)fminf((mx - z) * per_step, (float)(kSmSteps - 1)); };  // the last one is open below
+    auto clear_steps = [&]() {
+        for (int i = tid; i < 2 * kSmSteps; i += NT) steps[i] = 0;
+        __syncthreads();
+    };
+    bool counted = false;
     // ---- the short way
     const int most = min(kSmGuess, 2 * NT * (int)row.cluster);  // (at most half of the maxima: the bound stays high)
     if (p.vocab > kSmList && (f.k_on ? f.k <= most : f.p_on || f.m_on)) {
@@ -785,12 +804,17 @@ __global__ void __launch_bounds__(NT, NT == 256 ? 4 : 1) sample_kernel(const Sam
                         if (at < part) row.send(list + 8 * at, sm_key(z[e]), i + e);
                     }
             };
-            if (all)
+            if (all) {
+                clear_steps();
+                counted = true;
                 row.each([&](int i, const float(&z)[4], int m) {
                     total += m == 4 ? (row.weight(z[0]) + row.weight(z[1])) + (row.weight(z[2]) + row.weight(z[3])) : row.weight(z[0]);
+#pragma unroll
+                    for (int e = 0; e < 4; e++)
+                        if (e < m) atomicAdd(&steps[step_of(z[e])], 1);
                     pick(i, z, m);
                 });
-            else
+            } else
                 row.each(pick);
             if (all) total = row.block_sum_d(total);
             __syncthreads();
@@ -812,6 +836,7 @@ __global__ void __launch_bounds__(NT, NT == 256 ? 4 : 1) sample_kernel(const Sam
                 }
             }
             from[kSmMaxCluster] = n;
+            known.total = total;
             if (fits && (!f.k_on || n >= f.k)) {  // (n < k: roundings wider than the buckets)
                 bool done = true;
                 double mass = 0.0;
@@ -821,7 +846,20 @@ __global__ void __launch_bounds__(NT, NT == 256 ? 4 : 1) sample_kernel(const Sam
                     for (int k = 0; k < kSmMaxCluster; k++)
                         for (int i = tid; i < from[k + 1] - from[k]; i += NT) key[from[k] + i] = raw[k * part + i];
                     __syncthreads();
+                    // (the list's sums would overwrite the counts: they wait in registers)
+                    constexpr int KEEP = kSmSteps / NT;
+                    int kept[KEEP];
+#pragma unroll
+                    for (int k = 0; k < KEEP; k++) kept[k] = all ? steps[k * NT + tid] : 0;
                     done = sm_finish_list(row, p, r, f, n, all, f.p * total, all, &mass);
+                    if (!done) {
+                        __syncthreads();
+#pragma unroll
+                        for (int k = 0; k < KEEP; k++) {
+                            steps[k * NT + tid] = kept[k];
+                            all_steps[k * NT + tid] = 0;
+                        }
+                    }
                 }
                 if (!all) return;  // (the list holds all that top-k, or min-p, keeps)
                 if (tid == 0) {
@@ -831,7 +869,6 @@ __global__ void __launch_bounds__(NT, NT == 256 ? 4 : 1) sample_kernel(const Sam
                 const auto verdict = row.share(2);
                 if (verdict[0][0] != 0.0) return;
                 // top-p reaches further down: the long way begins below the list
-                known.total = total;
                 known.range = SampleRange{kSmKeyLowest, lo - 1, n, verdict[0][1], 0};
                 known.on = lo > kSmKeyLowest;
             }
@@ -911,18 +948,168 @@ __global__ void __launch_bounds__(NT, NT == 256 ? 4 : 1) sample_kernel(const Sam
         return 2;
     };
 
+    // The middle way: false where the steps cannot tell, or told wrongly.
+    auto bracket = [&](auto mass, double goal, SampleBorder &found) -> bool {
+        constexpr bool MASS = decltype(mass)::value;
+        row.share(1);  // (every block's counts are there, the first block's sums are clear)
+        const uint32_t to = mapa_u32(smem_u32(all_steps), 0);
+        for (int i = tid; i < kSmSteps; i += NT)
+            if (steps[i]) asm volatile("red.shared::cluster.add.u32 [%0], %1;" ::"r"(to + 4 * i), "r"(steps[i]) : "memory");
+        if (row.cluster == 1) __syncthreads();
+        else cluster_sync_all();
+        if (row.rank == 0) {
+            // running sums over the steps; warp 0 alone, 32 steps a time
+            if (tid < 32) {
+                double base = 0.0;
+                int at = -1, listed = 0, seen = 0;  // the first step behind the short way's list, the values before it
+                if (MASS && known.on) {
+                    // the list's own mass is exact: a few heavy values in the middle of their steps would be half a step off
+                    listed = step_of(sm_value(known.range.hi)) + 1;
+                    base = known.range.above_w;
+                    for (int s = lane; s < listed; s += 32) seen += all_steps[s];
+                    seen = __reduce_add_sync(0xffffffffu, seen);
+                    base += (double)(seen - known.range.above_n) * row.weight(mx - (listed - 0.5f) / per_step);
+                    if (base >= goal) at = listed - 1;
+                }
+                for (int s0 = listed & ~31; s0 < kSmSteps && at < 0; s0 += 32) {
+                    const int c = s0 + lane >= listed ? all_steps[s0 + lane] : 0;
+                    double run = MASS ? c * row.weight(mx - (s0 + lane + 0.5f) / per_step) : (double)c;
+#pragma unroll
+                    for (int o = 1; o < 32; o <<= 1) {
+                        const double v = __shfl_up_sync(0xffffffffu, run, o);
+                        if (lane >= o) run += v;
+                    }
+                    const unsigned hit = __ballot_sync(0xffffffffu, base + run >= goal);
+                    if (hit) at = s0 + __ffs(hit) - 1;
+                    base += __shfl_sync(0xffffffffu, run, 31);
+                }
+                if (lane == 0) {
+                    int a = at, b = at;
+                    // by mass the border may lie in a neighbour: both, where they fit
+                    if (MASS && at > 0 && at < kSmSteps - 2 && all_steps[at - 1] + all_steps[at] + all_steps[at + 1] <= kSmList) {
+                        a--;
+                        b++;
+                    }
+                    const bool good = at >= 0 && at < kSmSteps - 1 && all_steps[at] <= kSmList;
+                    sh.local[0] = good ? a : -1;
+                    sh.local[1] = b;
+                }
+            }
+        }
+        const auto where = row.share(2);
+        const int a = (int)where[0][0], b = (int)where[0][1];
+        if (a < 0) return false;
+        const uint32_t slots = mapa_u32(smem_u32(&sh.slots), 0), list = mapa_u32(smem_u32(row.scratch), 0);
+        double above = 0.0;
+        int above_n = 0;
+        row.each([&](int i, const float(&z)[4], int m) {
+            int s[4];
+            bool any = false;
+#pragma unroll
+            for (int e = 0; e < 4; e++) {
+                s[e] = e < m ? step_of(z[e]) : kSmSteps;
+                any = any || s[e] < a;
+                above_n += s[e] < a;
+            }
+            if (MASS && any) {
+                double w[4];
+#pragma unroll
+                for (int e = 0; e < 4; e++) w[e] = s[e] < a ? row.weight(z[e]) : 0.0;
+                above += (w[0] + w[1]) + (w[2] + w[3]);
+            }
+#pragma unroll
+            for (int e = 0; e < 4; e++)
+                if (s[e] >= a && s[e] <= b) {
+                    unsigned slot;
+                    asm volatile("atom.shared::cluster.add.u32 %0, [%1], 1;" : "=r"(slot) : "r"(slots) : "memory");
+                    if (slot < kSmList) row.send(list + 8 * slot, sm_key(z[e]), i + e);
+                }
+        });
+        if (MASS) above = row.block_sum_d(above);
+        above_n = row.block_sum_i(above_n);
+        __syncthreads();
+        if (tid == 0) {
+            sh.local[0] = above;
+            sh.local[1] = above_n;
+        }
+        const auto buf = row.share(2);
+        above = 0.0;
+        long long before_n = 0;
+        for (uint32_t k = 0; k < row.cluster; k++) {
+            above += buf[k][0];
+            before_n += (long long)buf[k][1];
+        }
+        if (row.rank == 0) {
+            const int n = min((int)sh.slots, kSmList);
+            unsigned long long *key = reinterpret_cast<unsigned long long *>(row.scratch);
+            double *w = row.scratch + kSmList, *run = row.scratch + 2 * kSmList;
+            sm_sort(key, n);
+            int at;  // number of the list's values above the border
+            bool good;
+            if (MASS) {
+                for (int i = tid; i < n; i += NT) w[i] = row.weight(sm_value(~(uint32_t)(key[i] >> 32)));
+                __syncthreads();
+                sm_running<NT>(sh, w, run, n);
+                int before = 0;
+                for (int i = tid; i < n; i += NT) before += above + run[i] < goal;
+                at = row.block_sum_i(before);
+                good = at < n && (above < goal || before_n == 0);
+            } else {
+                at = (int)(goal - (double)before_n) - 1;
+                good = at >= 0 && at < n;
+            }
+            int same = 0, more = 0;  // ties up to the border, and beyond it
+            uint32_t tau = 0;
+            if (good) {
+                tau = ~(uint32_t)(key[at] >> 32);
+                for (int i = tid; i < n; i += NT) {
+                    const bool tie = (uint32_t)(key[i] >> 32) == ~tau;
+                    same += tie && i <= at;
+                    more += tie && i > at;
+                }
+            }
+            same = row.block_sum_i(same);
+            more = row.block_sum_i(more);
+            __syncthreads();
+            if (tid == 0) {
+                sh.local[0] = good;
+                sh.local[1] = tau;
+                sh.local[2] = same;
+                sh.local[3] = more;
+            }
+        }
+        const auto border_at = row.share(4);
+        if (border_at[0][0] == 0.0) return false;
+        found = SampleBorder{(uint32_t)border_at[0][1], (int)border_at[0][2], border_at[0][3] == 0.0};
+        return true;
+    };
+
     SampleRange range{kSmKeyLowest, key_top, 0, 0.0, p.vocab};
     bool listed = p.vocab <= kSmList, goal_known = false;
     double goal = 0.0;
     if (!listed && f.k_on) {
         goal = f.k;
-        if (narrow(std::false_type{}, goal, false, nullptr, range, border) == 1) listed = true;
+        if (f.k > most && low_max < mx && mx < INFINITY) {  // (else the short way has looked at them, and found too many)
+            clear_steps();
+            row.each([&](int, const float(&z)[4], int m) {
+#pragma unroll
+                for (int e = 0; e < 4; e++)
+                    if (e < m) atomicAdd(&steps[step_of(z[e])], 1);
+            });
+            bounded = bracket(std::false_type{}, goal, border);
+        }
+        if (bounded) {
+        } else if (narrow(std::false_type{}, goal, false, nullptr, range, border) == 1) listed = true;
         else bounded = true;
     }
     if (!listed && f.p_on) {
         SampleBorder other;
         range = known.on ? known.range : SampleRange{kSmKeyLowest, key_top, 0, 0.0, p.vocab};
         goal = f.p * known.total;
+        if (counted && mx < INFINITY && bracket(std::true_type{}, goal, other)) {
+            border = other;
+            bounded = true;
+        } else {
         const int how = narrow(std::true_type{}, goal, !known.on, bounded ? &border : nullptr, range, other);
         goal_known = true;
         if (how == 1) {
@@ -931,6 +1118,7 @@ __global__ void __launch_bounds__(NT, NT == 256 ? 4 : 1) sample_kernel(const Sam
             if (bounded && other.tau == border.tau) other.ties = min(other.ties, border.ties);
             border = other;  // (never below top-k's: masses were counted inside it)
             bounded = true;
+        }
         }
     }
     if (listed) {
