@@ -456,6 +456,30 @@ __global__ void __launch_bounds__(384, 1) attn_tree_mma_kernel(const __grid_cons
     if (!aligned && tid == 0) report(p.status, kStatusWaitExpired, 940);
     const bool work = aligned && w.start(p, lane);
     bool ok = true;
+    // the current item's queries by threads x of `threads`: all copies of a thread are under way at once
+    auto load_q = [&](int x, int threads) {
+        constexpr int CH = DH / 8;
+        const __nv_bfloat16 *q = reinterpret_cast<const __nv_bfloat16 *>(p.q);
+        const int row0 = w.rb * ROWS, rows = min(ROWS, w.s.n * p.G - row0), ch = x % CH;
+        const __nv_bfloat16 *base = q + w.b * p.qs[0] + w.h * p.G * p.qs[2] + ch * 8;
+#pragma unroll 4
+        for (int row = x / CH; row < Cfg::kQTiles * 128; row += threads / CH) {
+            const int node = ((row0 + row) * p.g_inverse) >> 16, g = row0 + row - node * p.G;
+            const uint32_t dst = q_s + (row >> 7) * Cfg::kTileBytes + (ch >> 3) * kHalfBytes + (row & 127) * 128 + (((ch & 7) ^ (row & 7)) << 4);
+            const __nv_bfloat16 *src = row < rows ? base + node * p.qs[1] + g * p.qs[2] : q;
+            if (p.q_vectors) {
+                asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(row < rows ? 16 : 0) : "memory");
+            } else {
+                uint32_t y[4] = {0, 0, 0, 0};
+                if (row < rows)
+#pragma unroll
+                    for (int k = 0; k < 4; k++)
+                        y[k] = (uint32_t)__bfloat16_as_ushort(src[2 * k]) | ((uint32_t)__bfloat16_as_ushort(src[2 * k + 1]) << 16);
+                asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(dst), "r"(y[0]), "r"(y[1]), "r"(y[2]), "r"(y[3]) : "memory");
+            }
+        }
+        asm volatile("cp.async.wait_all;" ::: "memory");
+    };
     // waits of a whole warp, its first lane looking
     auto wait = [&](uint32_t bar, int parity) {
         bool r = true;
@@ -598,41 +622,19 @@ __global__ void __launch_bounds__(384, 1) attn_tree_mma_kernel(const __grid_cons
     } else if (work && warp >= 10) {
         // ---- queries, parents, values that are not finite: 64 threads
         const int x = tid - 320;
-        const __nv_bfloat16 *q = reinterpret_cast<const __nv_bfloat16 *>(p.q);
         int c = 0, n = 0;
         do {
-            const int row0 = w.rb * ROWS, rows = min(ROWS, w.s.n * p.G - row0);
             const int parent = x < w.s.n ? p.parents[(size_t)w.b * p.N + x] : -1;
             if (n > 1) ok = wait(e_done(n - 2), (n - 2) >> 1);  // the buffers of the item before the last are free
             if (ok && n > 0) ok = wait(q_empty, n - 1);
             if (!ok) break;
-            // 64 threads are few: all their copies are under way at once (through registers, a few at a time, the first queries of
-            // a block took 14 us of 64 KB)
-            constexpr int CH = DH / 8, LOADS = Cfg::kQTiles * 128 * CH / 64, STEP = 64 / CH;
-            const int ch = x % CH;
-            const __nv_bfloat16 *base = q + w.b * p.qs[0] + w.h * p.G * p.qs[2] + ch * 8;
-#pragma unroll 4
-            for (int l = 0; l < LOADS; l++) {
-                const int row = x / CH + l * STEP, node = ((row0 + row) * p.g_inverse) >> 16, g = row0 + row - node * p.G;
-                const uint32_t dst = q_s + (row >> 7) * Cfg::kTileBytes + (ch >> 3) * kHalfBytes + (row & 127) * 128 + (((ch & 7) ^ (row & 7)) << 4);
-                const __nv_bfloat16 *src = row < rows ? base + node * p.qs[1] + g * p.qs[2] : q;
-                if (p.q_vectors) {
-                    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(row < rows ? 16 : 0) : "memory");
-                } else {
-                    uint32_t y[4] = {0, 0, 0, 0};
-                    if (row < rows)
-#pragma unroll
-                        for (int k = 0; k < 4; k++)
-                            y[k] = (uint32_t)__bfloat16_as_ushort(src[2 * k]) | ((uint32_t)__bfloat16_as_ushort(src[2 * k + 1]) << 16);
-                    asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(dst), "r"(y[0]), "r"(y[1]), "r"(y[2]), "r"(y[3]) : "memory");
-                }
-            }
-            asm volatile("cp.async.wait_all;" ::: "memory");
+            if (n > 0) load_q(x, 64);  // (the first item's come from the softmax warps, which have nothing else to do yet)
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
             // a bad parent counts as none
             if (x < w.s.n && (parent >= x || parent < -1)) report(p.status, kStatusBadTree, parent);
             parents_s[n & 1][x] = (signed char)(parent >= x || parent < -1 ? -1 : parent);
             if (x == 0) bad_s[n & 1] = 0;
+            if (n == 0) asm volatile("bar.sync 3, 320;" ::: "memory");
             asm volatile("bar.sync 2, 64;" ::: "memory");  // (both warps: bad_s is cleared before either marks a node)
             if (lane == 0) mbar_arrive(q_full(n));
             for (int t = w.t0; t < w.t1 && ok; t++, c++) {
@@ -686,6 +688,9 @@ __global__ void __launch_bounds__(384, 1) attn_tree_mma_kernel(const __grid_cons
         const uint32_t ts = t_s(i) + lanes;
         const float sc = p.scale_log2, grow = kTreeRescaleLog2 / sc;
         const uint64_t sc2 = pack_f32x2(sc, sc);
+        load_q(tid, 256);
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        asm volatile("bar.arrive 3, 320;" ::: "memory");
         auto wait_all = [&](uint32_t bar, int parity) { return (bool)__all_sync(0xffffffffu, mbar_wait(bar, parity & 1)); };
         int n = 0, sn = 0, on = 0, other_on = 0;
         do {
