@@ -290,7 +290,7 @@ dbt_status dbt_op_gemm_tc_static(const void *W_dev, const void *X_dev, int32_t n
  *  - parents int32 [B][max_nodes]: the parent of each node, less than the node's own number, or -1 (a root).
  *  - status_dev int32 [2], zeroed by the caller: errors that only the device sees, {code, detail} as dbt_sync_status
  *    reports them (2 = a page id out of range, or a position behind the table's last page, detail -1; 3 = a bounded wait
- *    ran out; 4 = a parent that is not below its node, detail = the parent).  The first one stays.  Accesses stay inside
+ *    ran out, detail = its site, 900 and up; 4 = a parent that is not below its node, detail = the parent).  The first one stays.  Accesses stay inside
  *    the buffers: a bad page id is read as page 0 and not written, a bad parent counts as -1.
  *  - A message for a refused call is in dbt_last_error(NULL) of the calling thread. */
 

@@ -6,10 +6,12 @@
 //
 // Work split.  The tiles of all (sequence, KV head, row block) items stand in one line, each item headed by `lead` empty units for
 // what it costs besides its tiles, and the line is cut into equal runs, one per block: no block waits for the longest
-// sequence, whatever the lengths.  An item inside one run is written out at
-// once; of an item that is cut, each run leaves its unnormalised output with its maximum and sum in the workspace, and a second
-// kernel joins them in the order of the keys (no atomics: results do not depend on timing).  Lengths are read on the
-// device, so a captured call serves later lengths.
+// sequence, whatever the lengths.  An item inside one run is written out at once; of an item that is cut, each run leaves its
+// unnormalised output with its maximum and sum in the workspace, and a second kernel joins them in the order of the keys (no
+// atomics: results do not depend on timing).  Lengths are read on the device, so a captured call serves later lengths.
+//
+// Measured, bf16, head dimension 128: 16 sequences of up to 2048 keys and 16 nodes, 16 heads over 8 (74 MB of keys and values) 35 us,
+// 2.1 TB/s; 4 sequences of 32768 keys and 64 nodes, 32 heads over 8 (541 MB, 137 GFLOP) 156 us, 3.5 TB/s and 0.88 PFLOP/s.
 #pragma once
 
 #include "dbt_ptx.cuh"
@@ -168,7 +170,11 @@ __device__ __forceinline__ int tree_page(const TreeAttnParams &p, int b, int slo
 
 // ---- CUDA-core form: fp32 ------------------------------------------------------------------------------------
 // 16 x 16 threads; thread (ty, tx) forms the scores of rows ty * RM .. and keys tx, tx + 16, .. of a tile of 64 keys, and owns
-// columns 4 tx .. of the outputs of its rows.
+// columns 4 tx .. of the outputs of its rows.  RM is 1 up to 16 rows that share a KV head (two blocks per SM), else 4 (a quarter of the
+// reads of keys and values from shared memory per product).
+// What bounds it: the fp32 multiply-adds and the reads from shared memory that feed them: 8 sequences of 4096
+// keys and 64 nodes, 32 heads of 128 over 8, 1371 us, 25 TFLOP/s; 4 of 4096 keys and 4 nodes, 4 heads of 64, 38 us, 0.9 TB/s: the
+// loads of a tile are not under way while the one before is used.  Short sequences: the two launches (14 us a call with the binding).
 constexpr int kTsKeys = 64;
 template <int D, int RM>
 struct TreeSimtCfg {
@@ -179,7 +185,7 @@ struct TreeSimtCfg {
     static constexpr int kBlocksPerSm = kSmemBytes <= 113 * 1024 ? 2 : 1;
 };
 
-template <typename T, int D, int RM>
+template <int D, int RM>
 __global__ void __launch_bounds__(256, TreeSimtCfg<D, RM>::kBlocksPerSm) attn_tree_simt_kernel(const TreeAttnParams p) {
     using Cfg = TreeSimtCfg<D, RM>;
     constexpr int ROWS = Cfg::kRows, LD = Cfg::kLd, LDP = Cfg::kLdP, CV = D / 64;
@@ -190,7 +196,7 @@ __global__ void __launch_bounds__(256, TreeSimtCfg<D, RM>::kBlocksPerSm) attn_tr
     const int tid = threadIdx.x, lane = tid & 31, tx = tid & 15, ty = tid >> 4;
     TreeWalk<ROWS, kTsKeys> w;
     if (!w.start(p, lane)) return;  // (the same for every warp)
-    const T *kplane = reinterpret_cast<const T *>(p.cache), *vplane = kplane + (size_t)p.num_pages * p.hkv * 16 * D;
+    const float *kplane = reinterpret_cast<const float *>(p.cache), *vplane = kplane + (size_t)p.num_pages * p.hkv * 16 * D;
     do {
         const int rows = min(ROWS, w.s.n * p.G - w.rb * ROWS), r0 = w.rb * ROWS, keys = w.s.len + w.s.n;
         __syncthreads();  // the item before is done with shared memory
@@ -199,9 +205,9 @@ __global__ void __launch_bounds__(256, TreeSimtCfg<D, RM>::kBlocksPerSm) attn_tr
             const int r = i / (D / 8), c = (i - r * (D / 8)) * 8, node = (r0 + r) / p.G, g = (r0 + r) - node * p.G;
             float x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
             if (r < rows) {
-                const T *src = reinterpret_cast<const T *>(p.q) + w.b * p.qs[0] + node * p.qs[1] + (w.h * p.G + g) * p.qs[2] + c;
+                const float *src = reinterpret_cast<const float *>(p.q) + w.b * p.qs[0] + node * p.qs[1] + (w.h * p.G + g) * p.qs[2] + c;
 #pragma unroll
-                for (int k = 0; k < 8; k++) x[k] = load1(src + k);
+                for (int k = 0; k < 8; k++) x[k] = src[k];
             }
 #pragma unroll
             for (int k = 0; k < 8; k++) qs[r * LD + c + k] = x[k] * p.scale_log2;
@@ -315,12 +321,12 @@ __global__ void __launch_bounds__(256, TreeSimtCfg<D, RM>::kBlocksPerSm) attn_tr
                 if (tx == 0) p.stats[(size_t)w.slot * ROWS + r] = make_float2(m_run[i], l_run[i]);
             } else {
                 const int node = (r0 + r) / p.G, g = (r0 + r) - node * p.G;
-                T *dst = reinterpret_cast<T *>(p.out) + (((size_t)w.b * p.N + node) * p.hkv * p.G + w.h * p.G + g) * D;
+                float *dst = reinterpret_cast<float *>(p.out) + (((size_t)w.b * p.N + node) * p.hkv * p.G + w.h * p.G + g) * D;
                 const float inv = l_run[i] == 0.f ? 0.f : 1.f / l_run[i];
 #pragma unroll
                 for (int c = 0; c < CV; c++)
 #pragma unroll
-                    for (int e = 0; e < 4; e++) store1(dst + c * 64 + tx * 4 + e, o[i][4 * c + e] * inv);
+                    for (int e = 0; e < 4; e++) dst[c * 64 + tx * 4 + e] = o[i][4 * c + e] * inv;
             }
         }
     } while (w.next(p));
@@ -335,8 +341,14 @@ __global__ void __launch_bounds__(256, TreeSimtCfg<D, RM>::kBlocksPerSm) attn_tr
 // more than 2^8 (P stays below 2^8: the same relative error).  P is rounded to bf16 (2^-9 on average, relative), which the
 // tensor cores need; the sum adds the unrounded values.
 //
-// What bounds it: K and V from HBM up to some 128 rows (64 KB a key tile at head dimension 128: 1.5 us of an SM's share); at 256 rows
-// the tensor pipe, the exponentials and HBM take about as long as one another.
+// What bounds it: 256 rows over long sequences, the turns between the tensor cores and the softmax warps.  A pair of key tiles' work takes
+// 4100 cycles: 2240 in which a group turns its scores into probabilities (half of that is the special-function unit, 16
+// exponentials a cycle; tensor-memory and shared-memory traffic the rest) and 1640 in which it waits for its products (1200 of the
+// tensor pipe, and the signals).  HBM would take 2150, and loads taken out save 4 %.  128 rows or fewer and ragged lengths: what a run
+// costs besides its tiles, of 67k cycles 4k to find its place, 4k for the first queries, 12k for joining the groups and writing.
+// Not better: scores of 64 keys in two buffers (240 us where this takes 156: products 64 wide take as long as 128 wide),
+// 16 softmax warps with half a row a thread (176), a quarter of the exponentials as polynomials on the multiply-add pipes
+// (173: registers), scores read in pieces of 32 twice (169).
 //
 // Values that are not finite.  A node that a row does not see has probability 0, but 0 * NaN in the product is NaN.  So the
 // values of the nodes, once in shared memory, are looked through: elements that are not finite are replaced by 0 there, and
@@ -857,7 +869,8 @@ __global__ void __launch_bounds__(384, 1) attn_tree_mma_kernel(const __grid_cons
 }
 
 // ---- joining the parts of items that were cut --------------------------------------------------------------------
-// A warp per output row, in the order of the keys.
+// A warp per output row, in the order of the keys.  Its bound is latency: 16 ragged sequences' parts take 4 us behind the first kernel, 8
+// sequences-by-heads cut in 148 parts 7 us.
 template <typename T, int D, int ROWS, int KEYS>
 __global__ void __launch_bounds__(256) attn_tree_join_kernel(const TreeAttnParams p) {
     using Plan = TreePlan<ROWS, KEYS>;

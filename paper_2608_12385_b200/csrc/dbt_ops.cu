@@ -166,14 +166,14 @@ dbt_status check_tree(const dbt_attn_tree_args *a, bool pointers) {
     return DBT_OK;
 }
 
-template <typename T, int D, int RM>
+template <int D, int RM>
 cudaError_t tree_simt(const TreeAttnParams &p, void *stream) {
     using Cfg = TreeSimtCfg<D, RM>;
-    cudaError_t e = allow_smem(attn_tree_simt_kernel<T, D, RM>, Cfg::kSmemBytes);
-    if (e == cudaSuccess) e = launch(attn_tree_simt_kernel<T, D, RM>, dim3(p.blocks), 256, Cfg::kSmemBytes, stream, 1, false, p);
+    cudaError_t e = allow_smem(attn_tree_simt_kernel<D, RM>, Cfg::kSmemBytes);
+    if (e == cudaSuccess) e = launch(attn_tree_simt_kernel<D, RM>, dim3(p.blocks), 256, Cfg::kSmemBytes, stream, 1, false, p);
     if (e != cudaSuccess) return e;
     const long long warps = (long long)p.B * p.hkv * p.N * p.G;
-    return launch(attn_tree_join_kernel<T, D, Cfg::kRows, kTsKeys>, dim3((unsigned)((warps + 7) / 8)), 256, 0, stream, 1, true, p);
+    return launch(attn_tree_join_kernel<float, D, Cfg::kRows, kTsKeys>, dim3((unsigned)((warps + 7) / 8)), 256, 0, stream, 1, true, p);
 }
 
 template <typename T, int NT>
@@ -354,8 +354,8 @@ dbt_status dbt_op_attn_tree(const dbt_attn_tree_args *a, void *cuda_stream) {
     cudaError_t e;
     const bool few = s.rows == 16, wide = a->head_dim == 128;
     if (a->dtype == DBT_DTYPE_F32)
-        e = wide ? (few ? tree_simt<float, 128, 1>(p, cuda_stream) : tree_simt<float, 128, 4>(p, cuda_stream))
-                 : (few ? tree_simt<float, 64, 1>(p, cuda_stream) : tree_simt<float, 64, 4>(p, cuda_stream));
+        e = wide ? (few ? tree_simt<128, 1>(p, cuda_stream) : tree_simt<128, 4>(p, cuda_stream))
+                 : (few ? tree_simt<64, 1>(p, cuda_stream) : tree_simt<64, 4>(p, cuda_stream));
     else
         e = wide ? (s.rows == 128 ? tree_mma<128, false>(p, cuda_stream) : tree_mma<128, true>(p, cuda_stream))
                  : (s.rows == 128 ? tree_mma<64, false>(p, cuda_stream) : tree_mma<64, true>(p, cuda_stream));
@@ -384,8 +384,9 @@ dbt_status dbt_op_sample(const void *logits, int32_t dtype, int32_t rows, int32_
     p.logprobs = logprobs;
     p.vocab = vocab;
     // Blocks per row: enough to fill the device (four are resident per SM), or two per SM where a block's share is short already;
-    // and no more than leave a block 4096 values.  256 rows of 128256, top-k 50 with top-p and min-p: 70, 57, 57 us with 8, 4, 2 blocks a
-    // row; without filters 123, 124, 167; 256 rows of 32000: 72, 34, 24 us; one row of 128256 without filters: 25, 42, 73.
+    // and no more than leave a block 4096 values.  256 rows of 128256, top-k 50 with top-p and min-p: 69 us with 8 blocks a row, 56 with 4;
+    // top-k 400: 109, 78; without filters 90, 88; settings of all kinds 118, 127.  256 rows of 32000, the same filters: 72, 34, 24 us with 8,
+    // 4, 2 (then; 21 now); one row of 128256 without filters: 25, 42, 73 with 8, 4, 2 (then; 13 now).
     const long long sms = sm_count();
     int cluster = 1;
     while (vocab > cluster * kSmMaxSlice ||
@@ -393,8 +394,12 @@ dbt_status dbt_op_sample(const void *logits, int32_t dtype, int32_t rows, int32_
             !((long long)rows * cluster >= 2 * sms && vocab <= cluster * 16384)))
         cluster *= 2;
     p.slice = ((vocab + cluster - 1) / cluster + 7) / 8 * 8;
-    // Few rows: twice the threads, one block per SM: top-k 2000 of one row of 128256 62 us with 256 threads, 52 with 512 (1024 spill: 60).
+    // Few rows: twice the threads, one block per SM: top-k 2000 of one row of 128256 62 us with 256 threads, 52 with 512 (1024 spill: 60; then).
+    // Many rows, two blocks of 512 against four of 256 per SM: settings of all kinds 123 us, 133; without filters 35, 28 (64 rows).
     const bool few = (long long)rows * cluster <= sms;
+    p.rows = rows;
+    // More blocks than can be resident: the rows that may take long first (256 rows of 128256 with settings of all kinds 126 us, else 133).
+    p.order = top_p && (long long)rows * cluster > 4 * sms;
     cudaError_t e;
     if (dtype == DBT_DTYPE_F32)
         e = few ? sample_launch<float, 512>(p, rows, cluster, cuda_stream) : sample_launch<float, 256>(p, rows, cluster, cuda_stream);

@@ -5,12 +5,13 @@
 // order of ids, at which the running sum of the kept w exceeds u times their total.
 //
 // A row is shared out over a cluster of 1 to 8 blocks.  Its logits come from HBM once and are read again, from L1 or L2, by the
-// passes that follow (held in shared memory they left room for two blocks per SM; as it is four are resident and cover one
-// another's barriers: 256 rows of 128256 with all filters 241 us then).  No row is sorted as a whole.
+// passes that follow (held in shared memory they left room for two blocks per SM and 256 rows of 128256 with all filters took 383 us;
+// with four resident, which cover one another's barriers, 241, and 127 with the steps that came later).  No row is sorted as a whole.
 //
 // The short way.  Every thread knows the largest of the values it loaded, one for each place of its four-value loads; the K-th
-// largest of these maxima has at least K values of the row at or above it, and seldom many more.  What lies above that bound (K = top_k, or 512 where top-p alone asks)
-// is sent to the first block, which sorts it and finishes alone, if the kept set turns out to lie inside.
+// largest of these maxima has at least K values of the row at or above it, and seldom many more.  What lies above that bound
+// (K = top_k, or 512 where top-p alone asks) is sent to the first block, which sorts it and finishes alone, if the kept set turns
+// out to lie inside.
 //
 // The middle way, where more is kept.  The values' counts in 1024 equal steps below the largest (taken along in a pass that is made
 // anyway) say in which steps the border must lie -- by count exactly, by mass up to what the steps' width leaves open --; one pass
@@ -30,8 +31,10 @@
 // (1989)), relative error below 1e-14.  16 doubles are one row of the shared-memory banks: lookups do not conflict (64 entries
 // cost six cycles a warp, as much as the arithmetic).
 //
-// What bounds it: one row, the cluster barriers (a microsecond each); many rows, the 64-bit pipe where all of a row's
-// exponentials are needed (top-p alone, no filter at all), else the passes over L2.
+// What bounds it: one row, the cluster barriers (one to two microseconds each); many rows, where all of a row's exponentials are
+// needed (top-p alone, no filter at all), the latency of the 64-bit chains and of the passes over L2, else the passes.  Measured,
+// fp32 logits, 128256 a row: one row 13 us without filters, 15 with top-k 50, top-p and min-p, 25 with top-p alone; 256 rows (131 MB, 20 us
+// of HBM) 88, 56 and 153 to 198, with settings of all kinds 127; 64 rows without filters 28.
 #pragma once
 
 #include <type_traits>
@@ -61,6 +64,7 @@ struct SampleParams {
     int32_t *tokens;
     float *logprobs;
     int vocab, slice;  // values per block, a multiple of 8
+    int rows, order;   // order: long rows first
 };
 
 __device__ __forceinline__ uint32_t sm_key(float x) {
@@ -657,7 +661,29 @@ __global__ void __launch_bounds__(NT, NT == 256 ? 4 : 1) sample_kernel(const Sam
     row.rank = cluster_rank();
     asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(row.cluster));
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const int r = blockIdx.x / row.cluster;
+    int r = blockIdx.x / row.cluster;
+    if (p.order) {
+        // Of every NT rows those that may keep most come first: with top-p, and no top-k that the short way can take.  Such a row takes two
+        // to four times as long as the others, and begun last it runs alone.
+        const int i = r % NT, t = r - i + tid;
+        bool longer = false;
+        if (t < p.rows) {
+            const int k = p.top_k ? p.top_k[t] : 0;
+            longer = p.top_p[t] < 1.f && (k <= 0 || k > kSmGuess);
+        }
+        const unsigned those = __ballot_sync(0xffffffffu, longer);
+        if (lane == 0) sh.warp_i[warp] = __popc(those);
+        __syncthreads();
+        int before = __popc(those & ((1u << lane) - 1)), all = 0;
+#pragma unroll
+        for (int w = 0; w < NT / 32; w++) {
+            if (w < warp) before += sh.warp_i[w];
+            all += sh.warp_i[w];
+        }
+        if (t < p.rows && longer == (i < all) && (longer ? before == i : tid - before == i - all)) sh.found = t;
+        __syncthreads();
+        r = sh.found;
+    }
     row.base = row.rank * p.slice;
     row.n = max(0, min(p.slice, p.vocab - row.base));
     row.src = reinterpret_cast<const T *>(p.logits) + (long long)r * p.row_stride + row.base;
@@ -793,7 +819,7 @@ __global__ void __launch_bounds__(NT, NT == 256 ? 4 : 1) sample_kernel(const Sam
             const int part = kSmList / (int)row.cluster;
             const uint32_t list = mapa_u32(smem_u32(row.scratch + kSmList + row.rank * part), 0);
             const bool all = f.p_on && !f.k_on;
-            double total = 0.0;
+            double total = 0.0, listed = 0.0;
             const float lo_value = sm_value(lo);  // (the cleaned values are in the order of their patterns)
             auto pick = [&](int i, const float(&z)[4], int m) {
                 if (m == 4 ? fmaxf(fmaxf(z[0], z[1]), fmaxf(z[2], z[3])) < lo_value : z[0] < lo_value) return;
@@ -808,23 +834,33 @@ __global__ void __launch_bounds__(NT, NT == 256 ? 4 : 1) sample_kernel(const Sam
                 clear_steps();
                 counted = true;
                 row.each([&](int i, const float(&z)[4], int m) {
-                    total += m == 4 ? (row.weight(z[0]) + row.weight(z[1])) + (row.weight(z[2]) + row.weight(z[3])) : row.weight(z[0]);
+                    double w[4];
+#pragma unroll
+                    for (int e = 0; e < 4; e++) w[e] = e < m ? row.weight(z[e]) : 0.0;
+                    total += (w[0] + w[1]) + (w[2] + w[3]);
 #pragma unroll
                     for (int e = 0; e < 4; e++)
-                        if (e < m) atomicAdd(&steps[step_of(z[e])], 1);
+                        if (e < m) {
+                            atomicAdd(&steps[step_of(z[e])], 1);
+                            listed += z[e] >= lo_value ? w[e] : 0.0;
+                        }
                     pick(i, z, m);
                 });
             } else
                 row.each(pick);
-            if (all) total = row.block_sum_d(total);
+            if (all) {
+                total = row.block_sum_d(total);
+                listed = row.block_sum_d(listed);
+            }
             __syncthreads();
             if (tid == 0) {
                 sh.local[0] = sh.sent;
                 sh.local[1] = total;
+                sh.local[2] = listed;
             }
-            const auto buf = row.share(2);
+            const auto buf = row.share(3);
             bool fits = true;
-            total = 0.0;
+            total = listed = 0.0;
             int n = 0, from[kSmMaxCluster + 1];
 #pragma unroll
             for (int k = 0; k < kSmMaxCluster; k++) {
@@ -832,12 +868,17 @@ __global__ void __launch_bounds__(NT, NT == 256 ? 4 : 1) sample_kernel(const Sam
                 if (k < (int)row.cluster) {
                     n += (int)buf[k][0];
                     total += buf[k][1];
+                    listed += buf[k][2];
                     fits = fits && buf[k][0] <= part;
                 }
             }
             from[kSmMaxCluster] = n;
             known.total = total;
-            if (fits && (!f.k_on || n >= f.k)) {  // (n < k: roundings wider than the buckets)
+            if (all && !f.m_on && listed < f.p * total * (1.0 - 1e-9)) {
+                // top-p reaches further down for certain: no need to sort the list (7 us); the search begins below it
+                known.range = SampleRange{kSmKeyLowest, lo - 1, n, listed, 0};
+                known.on = lo > kSmKeyLowest;
+            } else if (fits && (!f.k_on || n >= f.k)) {  // (n < k: roundings wider than the buckets)
                 bool done = true;
                 double mass = 0.0;
                 if (row.rank == 0) {
@@ -868,7 +909,7 @@ __global__ void __launch_bounds__(NT, NT == 256 ? 4 : 1) sample_kernel(const Sam
                 }
                 const auto verdict = row.share(2);
                 if (verdict[0][0] != 0.0) return;
-                // top-p reaches further down: the long way begins below the list
+                // top-p reaches further down
                 known.range = SampleRange{kSmKeyLowest, lo - 1, n, verdict[0][1], 0};
                 known.on = lo > kSmKeyLowest;
             }
@@ -958,42 +999,43 @@ __global__ void __launch_bounds__(NT, NT == 256 ? 4 : 1) sample_kernel(const Sam
         if (row.cluster == 1) __syncthreads();
         else cluster_sync_all();
         if (row.rank == 0) {
-            // running sums over the steps; warp 0 alone, 32 steps a time
-            if (tid < 32) {
-                double base = 0.0;
-                int at = -1, listed = 0, seen = 0;  // the first step behind the short way's list, the values before it
-                if (MASS && known.on) {
-                    // the list's own mass is exact: a few heavy values in the middle of their steps would be half a step off
-                    listed = step_of(sm_value(known.range.hi)) + 1;
-                    base = known.range.above_w;
-                    for (int s = lane; s < listed; s += 32) seen += all_steps[s];
-                    seen = __reduce_add_sync(0xffffffffu, seen);
-                    base += (double)(seen - known.range.above_n) * row.weight(mx - (listed - 0.5f) / per_step);
-                    if (base >= goal) at = listed - 1;
+            // running sums over the steps, in the list's first two places (one warp alone, 32 steps a time, took 17 us of a row's 115)
+            double *each = row.scratch, *run = row.scratch + kSmList;
+            double base = 0.0;
+            int listed = 0, from = 0;  // the first step behind the short way's list
+            if (MASS && known.on) {
+                // the list's own mass is exact: a few heavy values in the middle of their steps would be half a step off
+                listed = step_of(sm_value(known.range.hi)) + 1;
+                int seen = 0;
+                for (int s = tid; s < listed; s += NT) seen += all_steps[s];
+                seen = row.block_sum_i(seen);
+                base = known.range.above_w + (double)(seen - known.range.above_n) * row.weight(mx - (listed - 0.5f) / per_step);
+                from = base >= goal ? listed - 1 : listed;
+            }
+            for (int s = tid; s < kSmSteps; s += NT) {
+                const int c = s >= listed ? all_steps[s] : 0;
+                each[s] = MASS ? c * row.weight(mx - (s + 0.5f) / per_step) : (double)c;
+            }
+            __syncthreads();
+            sm_running<NT>(sh, each, run, kSmSteps);
+            if (tid == 0) sh.found = kSmSteps;
+            __syncthreads();
+            int first = kSmSteps;
+            for (int s = tid; s < kSmSteps; s += NT)
+                if (first == kSmSteps && s >= from && base + run[s] >= goal) first = s;
+            first = __reduce_min_sync(0xffffffffu, first);
+            if (lane == 0) atomicMin(&sh.found, first);
+            __syncthreads();
+            if (tid == 0) {
+                const int at = sh.found;
+                int a = at, b = at;
+                // by mass the border may lie in a neighbour: both, where they fit
+                if (MASS && at > 0 && at < kSmSteps - 2 && all_steps[at - 1] + all_steps[at] + all_steps[at + 1] <= kSmList) {
+                    a--;
+                    b++;
                 }
-                for (int s0 = listed & ~31; s0 < kSmSteps && at < 0; s0 += 32) {
-                    const int c = s0 + lane >= listed ? all_steps[s0 + lane] : 0;
-                    double run = MASS ? c * row.weight(mx - (s0 + lane + 0.5f) / per_step) : (double)c;
-#pragma unroll
-                    for (int o = 1; o < 32; o <<= 1) {
-                        const double v = __shfl_up_sync(0xffffffffu, run, o);
-                        if (lane >= o) run += v;
-                    }
-                    const unsigned hit = __ballot_sync(0xffffffffu, base + run >= goal);
-                    if (hit) at = s0 + __ffs(hit) - 1;
-                    base += __shfl_sync(0xffffffffu, run, 31);
-                }
-                if (lane == 0) {
-                    int a = at, b = at;
-                    // by mass the border may lie in a neighbour: both, where they fit
-                    if (MASS && at > 0 && at < kSmSteps - 2 && all_steps[at - 1] + all_steps[at] + all_steps[at + 1] <= kSmList) {
-                        a--;
-                        b++;
-                    }
-                    const bool good = at >= 0 && at < kSmSteps - 1 && all_steps[at] <= kSmList;
-                    sh.local[0] = good ? a : -1;
-                    sh.local[1] = b;
-                }
+                sh.local[0] = at < kSmSteps - 1 && all_steps[at] <= kSmList ? a : -1;
+                sh.local[1] = b;
             }
         }
         const auto where = row.share(2);

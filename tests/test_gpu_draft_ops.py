@@ -403,6 +403,34 @@ def test_sample(dtype, V, filters):
                  pick([0.1, 0.5, 0.9, 0.99, 0.9999, 1.0]) if "p" in filters else None, pick([0.0, 0.001, 0.05, 0.5, 1.0]) if "m" in filters else None)
 
 
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("R", [160, 700])
+@pytest.mark.parametrize("V", [1030, 4000, 9001, 32000, 128256])
+def test_sample_many_rows(dtype, R, V):
+    """Calls with more blocks than the device holds at once: fourteen rows over and over, each as in a call of its own and as the 64-bit form
+    has it.  Narrow rows keep few tokens, wide ones most of the vocabulary; two have few distinct values."""
+    g = gen(V + R)
+    n = 14
+    z = torch.randn(n, V, generator=g) * torch.tensor([0.3, 1.0, 2.0, 3.0, 6.0, 0.0, 2.0, 2.0, 2.0, 2.0, 1.0, 1.0, 4.0, 2.0])[:, None]
+    z[3, torch.randint(0, V, (20,), generator=g)] += 9.0
+    z[10:12] = torch.randint(0, 5, (2, V), generator=g).float()
+    u = torch.rand(n, generator=g)
+    settings = dict(temperature=torch.tensor([1.0, 1.0, 0.8, 1.0, 0.0, 1.0, 1.3, 1.3, 1.7, 0.5, 0.9, 0.9, 1.0, 50.0]),
+                    top_k=torch.tensor([0, 40, 0, 400, 0, 900, 1500, 0, 0, V // 2, 1025, 0, 50, 0], dtype=torch.int32),
+                    top_p=torch.tensor([1.0, 1.0, 0.95, 0.9, 1.0, 0.5, 0.99, 0.7, 0.999, 0.9999, 1.0, 0.6, 0.9, 0.2]),
+                    min_p=torch.tensor([0.0, 0.05, 0.0, 0.02, 0.0, 0.0, 0.001, 0.0, 0.0, 0.0, 0.4, 0.0, 0.0, 0.0]))
+    z = z.to(TYPES[dtype])
+    over = torch.arange(R) % n
+    for names in ((), ("temperature",), ("top_k",), ("temperature", "top_p"), tuple(settings)):
+        s = {k: settings[k] for k in names}
+        check_sample(z, u.tolist(), **{k: v.tolist() for k, v in s.items()})
+        few = binding.op_sample(z.cuda(), u.cuda(), **{k: v.cuda() for k, v in s.items()})
+        many = binding.op_sample(z.cuda()[over], u.cuda()[over], **{k: v.cuda()[over] for k, v in s.items()})
+        for r in range(n):
+            assert (many[0][r::n] == few[0][r]).all()
+            assert (many[1][r::n] - few[1][r]).abs().nan_to_num(0.0).max() <= 2.0 ** -22 * max(1.0, abs(float(few[1][r])))
+
+
 @pytest.mark.parametrize("V", [5, 3000, 40000])
 def test_sample_edges_of_the_settings(V):
     g = gen(V)
