@@ -290,8 +290,8 @@ dbt_status dbt_op_gemm_tc_static(const void *W_dev, const void *X_dev, int32_t n
  *  - parents int32 [B][max_nodes]: the parent of each node, less than the node's own number, or -1 (a root).
  *  - status_dev int32 [2], zeroed by the caller: errors that only the device sees, {code, detail} as dbt_sync_status
  *    reports them (2 = a page id out of range, or a position behind the table's last page, detail -1; 3 = a bounded wait
- *    ran out, detail = its site, 900 and up; 4 = a parent that is not below its node, detail = the parent).  The first one stays.  Accesses stay inside
- *    the buffers: a bad page id is read as page 0 and not written, a bad parent counts as -1.
+ *    ran out, detail = its site, 900 and up; 4 = a parent that is not below its node, detail = the parent).  The first
+ *    one stays.  Accesses stay inside the buffers: a bad page id is read as page 0 and not written, a bad parent counts as -1.
  *  - A message for a refused call is in dbt_last_error(NULL) of the calling thread. */
 
 /* Frequencies (angle per position) of the rot_dim / 2 rotated pairs, HOST double [rot_dim / 2], and the factor on rotated
@@ -374,6 +374,7 @@ dbt_status dbt_op_attn_tree(const dbt_attn_tree_args *args_host, void *cuda_stre
  * The likeliest token always stays.  The token is the first, in rising order of ids, at which the running sum of the
  * remaining w exceeds u times their total.  temperature <= 0: the largest logit.  NaN logits count as -inf; a row without
  * any logit above -inf gives token -1 and log-probability -inf; where the largest is +inf, the infinite ones share all mass.
+ * u below 0 counts as 0; at 1, above it or not a number the last token that is kept comes.
  * temperature, top_p, min_p fp32 [rows], top_k int32 [rows]; each may be NULL (1, off, off, off).  tokens int32 [rows];
  * logprobs fp32 [rows] or NULL: log of the token's share of the remaining mass (0 where the temperature is <= 0).
  * Masses are formed and summed in 64 bits.  2 <= vocab <= 262144. */

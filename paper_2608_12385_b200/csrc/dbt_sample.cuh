@@ -90,7 +90,8 @@ struct SampleShared {
             int local[kSmMaxBuckets], all[kSmMaxCluster][kSmMaxBuckets];  // short way: the threads' maxima by bucket
         } maxima;
         struct {
-            double sums[kSmMaxSlice / kSmRun];  // long way: kept mass and ties of the border, per run of ids
+            double mass[kSmMaxSlice / kSmRun];  // where many are kept: per run of ids the kept mass, its running sum, the border's ties
+            double sums[kSmMaxSlice / kSmRun];
             int ties[kSmMaxSlice / kSmRun];
         } runs;
     };
@@ -629,7 +630,7 @@ __device__ __forceinline__ bool sm_finish_list(SampleRow<T, NT> &row, const Samp
     __syncthreads();
     int first = kSmList, last = -1;
     for (int i = tid; i < keep; i += NT) {
-        if (first == kSmList && w[i] > target) first = i;
+        if (first == kSmList && w[i] > target && wi[i] > 0.0) first = i;
         if (wi[i] > 0.0) last = i;
     }
     if (first < kSmList) atomicMin(&sh.found, first);
@@ -699,6 +700,7 @@ __global__ void __launch_bounds__(NT, NT == 256 ? 4 : 1) sample_kernel(const Sam
     SampleFilters f;
     const float temp = p.temperature ? p.temperature[r] : 1.f;
     f.u = p.uniforms[r];
+    if (f.u < 0.0) f.u = 0.0;  // (below nothing: the first token of any weight)
     f.k = p.top_k ? p.top_k[r] : 0;
     f.p = p.top_p ? p.top_p[r] : 1.f;
     f.m = p.min_p ? p.min_p[r] : 0.f;
@@ -1249,13 +1251,13 @@ __global__ void __launch_bounds__(NT, NT == 256 ? 4 : 1) sample_kernel(const Sam
         double mine = ((w[0] + w[1]) + (w[2] + w[3])) + ((w[4] + w[5]) + (w[6] + w[7]));
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) mine += __shfl_xor_sync(0xffffffffu, mine, o);
-        if (lane == 0) sh.runs.sums[q] = mine;
+        if (lane == 0) sh.runs.mass[q] = mine;
     }
     __syncthreads();
     if (warp == 0) {  // running sums of the runs
         double base = 0.0;
         for (int q0 = 0; q0 < runs; q0 += 32) {
-            double run = q0 + lane < runs ? sh.runs.sums[q0 + lane] : 0.0;
+            double run = q0 + lane < runs ? sh.runs.mass[q0 + lane] : 0.0;
 #pragma unroll
             for (int o = 1; o < 32; o <<= 1) {
                 const double v = __shfl_up_sync(0xffffffffu, run, o);
@@ -1285,8 +1287,8 @@ __global__ void __launch_bounds__(NT, NT == 256 ? 4 : 1) sample_kernel(const Sam
     int q = -1, q_last = 0;
     for (int q0 = 0; q0 < runs && q < 0; q0 += 32) {
         const int mine = q0 + lane;
-        const double s = mine < runs ? sh.runs.sums[mine] : 0.0, s0 = mine > 0 && mine < runs ? sh.runs.sums[mine - 1] : 0.0;
-        const unsigned hit = __ballot_sync(0xffffffffu, mine < runs && base + s > target), any = __ballot_sync(0xffffffffu, mine < runs && s > s0);
+        const bool some = mine < runs && sh.runs.mass[mine] > 0.0;  // (the running sums may rise by a rounding where there is nothing)
+        const unsigned hit = __ballot_sync(0xffffffffu, some && base + sh.runs.sums[mine] > target), any = __ballot_sync(0xffffffffu, some);
         if (any) q_last = q0 + 31 - __clz(any);
         if (hit) q = q0 + __ffs(hit) - 1;
     }

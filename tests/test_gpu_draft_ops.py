@@ -440,6 +440,18 @@ def test_sample_edges_of_the_settings(V):
                  [0.0] * 9 + [2.0, 1.0, 0.0])
 
 
+@pytest.mark.parametrize("V", [5, 3000, 40000])
+@pytest.mark.parametrize("filters", [dict(), dict(top_k=[3] * 4), dict(top_p=[0.999] * 4), dict(top_k=[2500] * 4)])
+def test_sample_numbers_outside_their_range(V, filters):
+    """Below zero: the first token that is kept; above one, or not a number: the last.  Ids at both ends weigh nothing."""
+    z = (torch.randn(1, V, generator=gen(V)) * 2).repeat(4, 1)
+    z[:, : V // 3] = -math.inf
+    z[:, V - V // 3 :] = -math.inf
+    want = check_sample(z, [0.0, 0.0, 2.0, math.nan], **filters)
+    dev = {k: torch.as_tensor(v, dtype=torch.int32 if k == "top_k" else torch.float32).cuda() for k, v in filters.items()}
+    assert binding.op_sample(z.cuda(), torch.tensor([-1.0, -math.inf, math.inf, math.nan]).cuda(), **dev)[0].tolist() == want
+
+
 @pytest.mark.parametrize("V", [6, 2000, 50000])
 def test_sample_rows_without_anything_and_with_infinities(V):
     inf, nan = math.inf, math.nan
