@@ -34,7 +34,7 @@
 // What bounds it: one row, the cluster barriers (one to two microseconds each); many rows, where all of a row's exponentials are
 // needed (top-p alone, no filter at all), the latency of the 64-bit chains and of the passes over L2, else the passes.  Measured,
 // fp32 logits, 128256 a row: one row 13 us without filters, 15 with top-k 50, top-p and min-p, 25 with top-p alone; 256 rows (131 MB, 20 us
-// of HBM) 88, 56 and 153 to 198, with settings of all kinds 127; 64 rows without filters 28.
+// of HBM) 88, 56 and 153 to 198, with settings of all kinds 127 to 130; 64 rows without filters 28.
 #pragma once
 
 #include <type_traits>
