@@ -273,6 +273,18 @@ def test_attn_tree_long_ragged_batch(dtype):
 
 
 @pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("B,D,nq,nkv,N,far", [(150, 64, 8, 4, 5, 300), (1000, 128, 2, 1, 2, 40), (70, 128, 64, 4, 21, 400), (40, 64, 32, 2, 64, 200), (333, 64, 4, 4, 1, 700)])
+def test_attn_tree_more_items_than_blocks(dtype, B, D, nq, nkv, N, far):
+    """Several whole items in a block's run, more sequences than a warp looks through at once, several row blocks an item, sequences without
+    nodes between."""
+    g = gen(B)
+    lens = torch.randint(0, far, (B,), generator=g).tolist()
+    counts = torch.randint(0, N + 1, (B,), generator=g).tolist()
+    lens[3], counts[3], lens[5], counts[5], counts[7], counts[8] = 0, N, 128, N, 0, 0
+    run_attention(dtype, D, nq, nkv, N, lens, counts, "random", seed=B + 1)
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
 @pytest.mark.parametrize("what", [math.nan, math.inf, -math.inf])
 def test_attn_tree_nodes_that_a_row_does_not_see_may_hold_anything(dtype, what):
     """Two branches below the root; the second branch's keys and values are not finite.  Rows of the first do not change."""
