@@ -10,7 +10,7 @@
 //
 // The short way.  Every thread knows the largest of the values it loaded, one for each place of its four-value loads; the K-th
 // largest of these maxima has at least K values of the row at or above it, and seldom many more.  What lies above that bound
-// (K = top_k, or 512 where top-p alone asks) is sent to the first block, which sorts it and finishes alone, if the kept set turns
+// (K = top_k, or 384 where top-p alone asks) is sent to the first block, which sorts it and finishes alone, if the kept set turns
 // out to lie inside.
 //
 // The middle way, where more is kept.  The values' counts in 1024 equal steps below the largest (taken along in a pass that is made
@@ -33,8 +33,8 @@
 //
 // What bounds it: one row, the cluster barriers (one to two microseconds each); many rows, where all of a row's exponentials are
 // needed (top-p alone, no filter at all), the latency of the 64-bit chains and of the passes over L2, else the passes.  Measured,
-// fp32 logits, 128256 a row: one row 13 us without filters, 15 with top-k 50, top-p and min-p, 25 with top-p alone; 256 rows (131 MB, 20 us
-// of HBM) 88, 56 and 153 to 198, with settings of all kinds 127 to 130; 64 rows without filters 28.
+// fp32 logits, 128256 a row: one row 13 us without filters, 15 with top-k 50, top-p and min-p, 23 with top-p alone; 256 rows (131 MB, 20 us
+// of HBM) 88, 56 and 137 to 191, with settings of all kinds 125 to 129; 64 rows without filters 28.
 #pragma once
 
 #include <type_traits>
@@ -46,7 +46,11 @@ namespace dbt {
 constexpr int kSmBuckets = 16;   // of a round by count; by mass kSmMassBuckets
 constexpr int kSmMassBuckets = 8;
 constexpr int kSmList = 1024;    // values that one block sorts
-constexpr int kSmGuess = 512;    // values that the short way asks for where top-k does not say, and its largest top_k
+constexpr int kSmGuess = 512;    // the largest top_k of the short way
+// Values that the short way asks for where top-p alone says how many: a list of up to 512 is sorted in two thirds of the time that one
+// of up to 1024 takes.  With 512, 384, 256: one row of 32000 21.0, 19.0, 18.9 us; 64 rows of 128256 114, 85, 83; 256 rows whose
+// border lies below the list 295, 294, 383 (too few exact ones for the middle way).
+constexpr int kSmNucleus = 384;
 constexpr int kSmMaxBuckets = 64;  // for the threads' maxima
 constexpr int kSmRun = 256;      // ids summed together by a warp on the long way
 constexpr int kSmSteps = 1024;   // of the middle way
@@ -808,7 +812,7 @@ __global__ void __launch_bounds__(NT, NT == 256 ? 4 : 1) sample_kernel(const Sam
                 const int v = __shfl_up_sync(0xffffffffu, run, o);
                 if (lane >= o) run += v;
             }
-            const int want = f.k_on ? f.k : most;
+            const int want = f.k_on ? f.k : min(kSmNucleus, most);
             const unsigned at = __ballot_sync(0xffffffffu, run >= want);
             const int l = at ? __ffs(at) - 1 : 31, before = __shfl_sync(0xffffffffu, run - a - b, l), first = __shfl_sync(0xffffffffu, a, l);
             const int j = 2 * l + (before + first < want);
