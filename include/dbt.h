@@ -301,7 +301,8 @@ enum {
     DBT_ROPE_LINEAR = 1, /* base_i / factor: positions squeezed into the trained range */
     DBT_ROPE_BASE = 2,   /* base * factor^(rot_dim / (rot_dim - 2)) for base: the slowest pair slows by factor, the fastest keeps */
     DBT_ROPE_RAMP = 3,   /* pairs of at most `low` turns over trained_len slow by factor, of at least `high` turns keep, a linear ramp
-                            over the pairs between; the factor on queries and keys is 0.1 ln(factor) + 1 */
+                            over the pairs between, which begins at pair 0 at the earliest and ends at pair rot_dim - 1 at the latest
+                            (behind the last pair where that one makes more than `low` turns); the factor on queries and keys is 0.1 ln(factor) + 1 */
     DBT_ROPE_BANDS = 4   /* by the turns over trained_len: up to `low` slow by factor, from `high` on keep, between them a blend
                             linear in the turns */
 };

@@ -217,16 +217,18 @@ dbt_status dbt_rope_frequencies(const dbt_rope_spec *s, double *freq, float *sca
     const double base = s->kind == DBT_ROPE_BASE ? s->base * std::pow(s->factor, rot / (rot - 2.0)) : s->base;
     // RAMP: the pair that makes `turns` turns over the trained length
     auto pair_of = [&](double turns) { return rot * std::log(s->trained_len / (turns * two_pi)) / (2.0 * std::log(s->base)); };
-    double first = 0.0, last = 1.0;
+    // The ramp's ends, the upper one at most rot - 1 (YaRN, Peng et al. 2023): it may lie behind the last pair, which then makes more than
+    // `low` turns and is slowed by a part.
+    double first = 0.0, last = 0.0;
     if (s->kind == DBT_ROPE_RAMP) {
         first = std::fmax(std::floor(pair_of(s->high)), 0.0);
-        last = std::fmin(std::ceil(pair_of(s->low)), pairs - 1.0);
+        last = std::fmin(std::ceil(pair_of(s->low)), rot - 1.0);
     }
     for (int i = 0; i < pairs; i++) {
         const double f = std::pow(base, -2.0 * i / rot);
         double slow = 0.0;  // share of the slowed frequency
         if (s->kind == DBT_ROPE_LINEAR) slow = 1.0;
-        if (s->kind == DBT_ROPE_RAMP) slow = std::fmin(1.0, std::fmax(0.0, (i - first) / std::fmax(last - first, 1e-3)));
+        if (s->kind == DBT_ROPE_RAMP) slow = i >= last ? 1.0 : i <= first ? 0.0 : (i - first) / (last - first);
         if (s->kind == DBT_ROPE_BANDS) slow = 1.0 - std::fmin(1.0, std::fmax(0.0, (s->trained_len * f / two_pi - s->low) / (s->high - s->low)));
         freq[i] = slow == 0.0 ? f : f / s->factor * slow + f * (1.0 - slow);
     }

@@ -227,6 +227,32 @@ def test_ramp_frequencies(lib):
     assert 0 < lo < hi < 63
 
 
+@pytest.mark.parametrize("rot,base,trained,low,high", [(128, 10000.0, 131072, 1, 32), (128, 10000.0, 65536, 1, 32), (8, 10000.0, 8192, 1, 32), (64, 10000.0, 1e9, 1, 32),
+                                                       (64, 10000.0, 1e14, 1, 2), (128, 10000.0, 8192, 1, 32), (128, 500000.0, 8192, 1, 32),
+                                                       (64, 10000.0, 128, 1, 32), (64, 10000.0, 128, 32, 64), (64, 10000.0, 6, 1, 2), (2, 10000.0, 8192, 1, 32)])
+def test_ramp_slows_each_pair_by_its_own_turns(lib, rot, base, trained, low, high):
+    """Pairs of at most `low` turns slow by the whole factor and no others do, those of at least `high` keep; between them the ramp of
+    the published method (YaRN, Peng et al. 2023), whose upper end is at most rot - 1: beyond the last pair where that one still makes
+    more than `low` turns, and not cut to it."""
+    factor = 16.0
+    f, _ = binding.rope_frequencies(rot, base, "ramp", factor=factor, trained_len=trained, low=low, high=high)
+    pair_of = lambda turns: rot * math.log(trained / (turns * 2 * math.pi)) / (2 * math.log(base))  # noqa: E731
+    lo, hi = max(math.floor(pair_of(high)), 0), min(math.ceil(pair_of(low)), rot - 1)
+    for i in range(rot // 2):
+        plain = base ** (-2 * i / rot)
+        turns = trained * plain / (2 * math.pi)
+        slow = 1.0 if i >= hi else 0.0 if i <= lo else (i - lo) / (hi - lo)
+        assert f[i].item() == pytest.approx(plain * (slow / factor + 1 - slow), rel=1e-12)
+        if turns <= low * (1 - 1e-12):
+            assert f[i].item() == pytest.approx(plain / factor, rel=1e-12)
+        elif turns >= high * (1 + 1e-12):
+            assert f[i].item() == pytest.approx(plain, rel=1e-12)
+        elif hi <= rot // 2 - 1:
+            continue  # (the ramp's ends are whole pairs: the one below `low` turns may be the last, the one above `high` the first)
+        else:
+            assert f[i].item() > plain / factor * (1 + 1e-9)  # more than `low` turns, and the end lies behind it
+
+
 def test_band_frequencies(lib):
     f, scale = binding.rope_frequencies(128, 500000.0, "bands", factor=8.0, trained_len=8192, low=1, high=4)
     p, _ = binding.rope_frequencies(128, 500000.0)
