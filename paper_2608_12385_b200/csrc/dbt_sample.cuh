@@ -709,7 +709,10 @@ __global__ void __launch_bounds__(NT, NT == 256 ? 4 : 1) sample_kernel(const Sam
     f.p = p.top_p ? p.top_p[r] : 1.f;
     f.m = p.min_p ? p.min_p[r] : 0.f;
     f.m_on = f.m > 0.0;
-    if (f.m > 1.0) f.k = 1;  // nothing but the likeliest token reaches it
+    if (f.m > 1.0) {  // no weight reaches it: the likeliest token stays alone, and is not held against it again
+        f.k = 1;
+        f.m_on = false;
+    }
     f.k_on = f.k > 0 && f.k < p.vocab;
     f.p_on = !(f.p >= 1.0);
     if (f.p != f.p) f.p = 0.0;

@@ -498,6 +498,20 @@ def test_sample_ties(V, distinct):
         check_sample(z, u, [0.9] * 9, **kw)
 
 
+@pytest.mark.parametrize("V", [1100, 2000, 40000, 262144])
+@pytest.mark.parametrize("settings", [dict(), dict(top_k=[2000] * 5), dict(top_p=[0.7] * 5), dict(top_k=[5] * 5, top_p=[0.3] * 5, temperature=[0.0, 0.5, 1.0, 3.0, math.inf])])
+def test_sample_min_p_above_one_leaves_the_likeliest_also_among_many_equal(V, settings):
+    """More equal largest logits than a list holds: the first of them is the only one that stays, whatever `min_p` above one says."""
+    z = torch.randn(5, V, generator=gen(V))
+    z[0] = 0.25
+    z[1, 17:1060] = 9.0
+    z[2, 17:1060] = math.inf
+    z[3, -1030:] = 9.0
+    for m in (float(np.nextafter(np.float32(1), np.float32(2))), 2.0, math.inf):
+        tok = check_sample(z, [0.0, 0.5, 1 - 2.0 ** -24, 0.3, 0.9], min_p=[m] * 5, **settings)
+        assert tok[:4] == [0, 17, 17, V - 1030]
+
+
 def test_sample_strided_and_odd_rows():
     g = gen(21)
     store = torch.randn(5, 1003, generator=g) * 2
