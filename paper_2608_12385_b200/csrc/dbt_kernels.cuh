@@ -878,14 +878,17 @@ __global__ void moe_lists_kernel(const int32_t *idx, int R, int kmax, int E, int
 }
 
 // Scores that the tokens of a step are drawn by: log(alpha p + (1 - alpha) mean_j q_j) (Eq. alpha, Eq. mixloss; Appendix C.1) from the
-// records of readout_stats_kernel, a CTA per (row, chunk).  A sampler's temperature then acts on the mixture itself.
+// records of readout_stats_kernel, a CTA per (row, chunk).  A sampler's temperature then acts on the mixture itself.  Formed from the paths'
+// logarithms, x_j = z_j - m_j - log d_j + log of the path's share, as max x + log sum e^(x_j - max x): as a probability a token 104 below the
+// largest would be 0 in fp32, and one 87 below a few bits, while a high temperature gives such tokens most of the mass.
 __global__ void __launch_bounds__(kRoThreads) mix_scores_kernel(const float *Z, int B, int V, int chunk, int P, const float *stats, float *scores) {
     pdl_enter();
-    __shared__ float glob[3 + 2 * kMaxBranches];  // m1, d1, alpha, then (m_j, d_j) per branch
+    __shared__ float top[1 + kMaxBranches], shift[1 + kMaxBranches];  // per path m_j; the path's share and normaliser as a logarithm
     const int b = blockIdx.x, ck = blockIdx.y, nc = gridDim.y, tid = threadIdx.x, lane = tid & 31;
     const int v0 = ck * chunk, v1 = min(V, v0 + chunk), nb = P - 1;
     if (tid < 32) {
         const float *rec = stats + (size_t)b * nc * kRoRec;
+        float alpha = 1.f;
         for (int j = 0; j <= nb; j++) {
             const int at = j == 0 ? 0 : 3 + 2 * j;
             float m = -INFINITY, s = 0.f, sq = 0.f;
@@ -898,20 +901,26 @@ __global__ void __launch_bounds__(kRoThreads) mix_scores_kernel(const float *Z, 
             }
             s = warp_sum(s);
             sq = warp_sum(sq);
+            if (j == 0) alpha = fminf(1.f, fmaxf(0.5f, sq / (s * s)));
             if (lane == 0) {
-                const int to = j == 0 ? 0 : 1 + 2 * j;
-                glob[to] = m;
-                glob[to + 1] = s;
-                if (j == 0) glob[2] = fminf(1.f, fmaxf(0.5f, sq / (s * s)));
+                top[j] = m;
+                shift[j] = logf(j == 0 ? alpha : (1.f - alpha) / (float)nb) - logf(s);  // (-inf for the branches where alpha is 1)
             }
         }
     }
     __syncthreads();
-    const float m1 = glob[0], d1 = glob[1], alpha = glob[2], inv_nb = 1.f / (float)nb;
     for (int v = v0 + tid; v < v1; v += kRoThreads) {
-        float q = 0.f;
-        for (int j = 0; j < nb; j++) q += expf(__ldcg(Z + (size_t)((j + 1) * B + b) * V + v) - glob[3 + 2 * j]) / glob[4 + 2 * j];
-        scores[(size_t)b * V + v] = logf(alpha * (expf(__ldcg(Z + (size_t)b * V + v) - m1) / d1) + (1.f - alpha) * (q * inv_nb));
+        float m = -INFINITY, s = 0.f;  // s is in units of e^m
+        for (int j = 0; j <= nb; j++) {
+            const float x = __ldcg(Z + (size_t)(j * B + b) * V + v) - top[j] + shift[j];
+            if (x > m) {
+                s = s * expf(m - x) + 1.f;
+                m = x;
+            } else if (x != -INFINITY) {  // (a logit that is not a number makes the score one)
+                s += expf(x - m);
+            }
+        }
+        scores[(size_t)b * V + v] = m + logf(s);
     }
 }
 

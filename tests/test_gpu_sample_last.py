@@ -81,6 +81,45 @@ def test_sampling_from_the_mixture(name):
     assert m.sync_status() == (0, 0)
 
 
+@pytest.mark.parametrize("name", ["bf16", "bf16-4-paths", "fp32"])
+@pytest.mark.parametrize("temperature", [1.0, 20.0, 80.0])
+def test_temperature_reaches_tokens_whose_probability_fp32_does_not_hold(name, temperature):
+    """Logits spread over some hundred, so that most probabilities are below the smallest number of fp32, while the temperature gives their
+    tokens most of the mass.
+
+    Every logit stands twice, so alpha is 0.5.  A score is a sum of a difference of logits (below 2^10 here), logarithms of sums and of alpha, and
+    one more logarithm: four roundings of at most 2^-15 each, and the sums' own 2^-19: below 2^-12.  The mass of a set moves by 2^-12 / T
+    relative, in numerator and denominator."""
+    cfg, B = CONFIGS[name], 4
+    weights = make_weights(cfg, seed=0, matrix_std=0.08)
+    head = weights["lm_head"]
+    half = cfg.vocab // 2
+    head[half:2 * half] = head[:half]
+    m = binding.Model(cfg, binding.weights_to_device(weights), B, 64)
+    tok = make_tokens(cfg, B, 12, seed=1).cuda()
+    spread = float(m.decode_full(tok[:, 0].contiguous())["z1"].std())
+    weights["lm_head"] = (head.float() * (60.0 / spread)).to(head.dtype)
+    m = binding.Model(cfg, binding.weights_to_device(weights), B, 64)
+    g, sure, far = torch.Generator().manual_seed(8), 0, 0
+    bound = 2 * 2.0 ** -12 / temperature
+    for t in range(12):
+        out = m.decode_full(tok[:, t].contiguous())
+        assert (out["alpha"] - 0.5).abs().max() <= 2.0 ** -20
+        scores = mixture_scores(out)
+        assert 150 < -scores.min() < 2 ** 10
+        u = torch.rand(B, generator=g)
+        drawn, logp = (x.tolist() for x in m.sample_last(u.cuda(), temperature=torch.full((B,), temperature, device="cuda")))
+        for b in range(B):
+            want, lp, near = ref.sample_row(scores[b], float(u[b]), temperature)
+            if near > bound:
+                sure += 1
+                far += scores[b][want] < -110
+                assert drawn[b] == want, (drawn[b], want, near)
+                assert abs(logp[b] - lp) <= bound + 2.0 ** -20
+    assert sure >= 24
+    assert temperature < 80 or far >= 12
+
+
 def test_sampling_after_primary_only_and_boundary_steps():
     cfg, B = CONFIGS["bf16"], 3
     m = model(cfg, B)
