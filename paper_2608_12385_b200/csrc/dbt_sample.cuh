@@ -665,6 +665,7 @@ __global__ void __launch_bounds__(NT, NT == 256 ? 4 : 1) sample_kernel(const Sam
     row.parity = 0;
     row.rank = cluster_rank();
     asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(row.cluster));
+    if (row.cluster > 1) cluster_arrive();  // waited for before the first store into another block's shared memory
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     int r = blockIdx.x / row.cluster;
     if (p.order) {
@@ -729,6 +730,7 @@ __global__ void __launch_bounds__(NT, NT == 256 ? 4 : 1) sample_kernel(const Sam
         sh.slots = 0;
     }
     if (tid < kSmMaxBuckets) sh.maxima.local[tid] = 0;
+    if (row.cluster > 1) cluster_wait();  // every block of the cluster runs: its shared memory may be written
     {
         const auto buf = row.share(2);
         for (uint32_t k = 0; k < row.cluster; k++) {

@@ -512,6 +512,23 @@ def test_sample_min_p_above_one_leaves_the_likeliest_also_among_many_equal(V, se
         assert tok[:4] == [0, 17, 17, V - 1030]
 
 
+@pytest.mark.parametrize("V,R", [(4100, 2000), (8200, 1500), (16500, 300), (33000, 1), (70000, 150)])
+def test_sample_clusters_whose_blocks_begin_at_different_times(V, R):
+    """More clusters of two, four and eight blocks than the device holds, of which many leave at once (rows without a number, temperature 0)
+    and make room for others: each row as in a call of its own, call after call."""
+    g = gen(V)
+    n = 5
+    z = torch.randn(n, V, generator=g) * 2
+    z[1] = -math.inf
+    u, t, k = torch.rand(n, generator=g), torch.tensor([1.0, 1.0, 0.0, 0.8, 1.0]), torch.tensor([0, 0, 0, 40, 1500], dtype=torch.int32)
+    want = check_sample(z, u.tolist(), temperature=t.tolist(), top_k=k.tolist())
+    over = torch.arange(R) % n
+    args = [x.cuda()[over] for x in (z, u, t, k)]
+    expected = torch.tensor(want, dtype=torch.int32).cuda()[over]
+    for _ in range(20):
+        assert torch.equal(binding.op_sample(*args)[0], expected)
+
+
 def test_sample_strided_and_odd_rows():
     g = gen(21)
     store = torch.randn(5, 1003, generator=g) * 2
