@@ -520,6 +520,23 @@ class Model:
         if st != DBT_OK:
             raise DbtError(st, self.L.dbt_last_error(self._h).decode())
 
+    def _own_stream(self) -> torch.cuda.Stream:
+        return self.stream if self.stream is not None else torch.cuda.default_stream(self.device)
+
+    def _elsewhere(self) -> bool:
+        """Whether the caller works on another stream than the model does."""
+        return _current_stream(self.device.index) != (self.stream.cuda_stream if self.stream is not None else 0)
+
+    def _empty(self, *shape, dtype) -> torch.Tensor:
+        """Memory for a result that the library writes on the model's stream.  It comes from that stream's share of the allocator: from the
+        current stream's, it could still be read by earlier work there, and be handed out again before the model's stream has written it."""
+        if not self._elsewhere():
+            return torch.empty(*shape, dtype=dtype, device=self.device)
+        with torch.cuda.stream(self._own_stream()):
+            t = torch.empty(*shape, dtype=dtype, device=self.device)
+        t.record_stream(torch.cuda.current_stream(self.device))  # (the caller reads it there)
+        return t
+
     def close(self):
         if getattr(self, "_h", None):
             torch.cuda.synchronize(self.device)
@@ -562,7 +579,7 @@ class Model:
     def prefill(self, tokens_dev: torch.Tensor, want_logits: bool = False):
         assert tokens_dev.dtype == torch.int32 and tokens_dev.is_cuda and tokens_dev.is_contiguous()
         B, n = tokens_dev.shape
-        out = torch.empty(B, self.cfg.vocab, dtype=torch.float32, device=self.device) if want_logits else None
+        out = self._empty(B, self.cfg.vocab, dtype=_F32) if want_logits else None
         self._check(self.L.dbt_prefill(self._h, tokens_dev.data_ptr(), B, n, _p(out)))
         return out
 
@@ -571,10 +588,8 @@ class Model:
         assert tokens_dev.dtype == torch.int32 and tokens_dev.is_cuda and tokens_dev.is_contiguous()
         B, S = tokens_dev.shape
         V, K = self.cfg.vocab, self.cfg.n_paths
-        out = {"next": torch.empty(B, dtype=torch.int32, device=self.device),
-               "z1": torch.empty(B, V, dtype=torch.float32, device=self.device),
-               "z2": torch.empty((B, V) if K == 2 else (K - 1, B, V), dtype=torch.float32, device=self.device),
-               "alpha": torch.empty(B, dtype=torch.float32, device=self.device)}
+        out = {"next": self._empty(B, dtype=_I32), "z1": self._empty(B, V, dtype=_F32),
+               "z2": self._empty(*((B, V) if K == 2 else (K - 1, B, V)), dtype=_F32), "alpha": self._empty(B, dtype=_F32)}
         self._check(self.L.dbt_prefill_boundary(self._h, tokens_dev.data_ptr(), B, S, _p(out["next"]), _p(out["z1"]),
                                                 _p(out["z2"]), _p(out["alpha"])))
         return out
@@ -591,14 +606,20 @@ class Model:
     def sample_last(self, uniforms: torch.Tensor, temperature: torch.Tensor | None = None, top_k: torch.Tensor | None = None,
                     top_p: torch.Tensor | None = None, min_p: torch.Tensor | None = None, next_dev: torch.Tensor | None = None):
         """Tokens of the last step (any of the step calls, or prefill_boundary) drawn from its mixture by the rules of op_sample instead of
-        picked: (tokens int32 [B], log of each token's share).  The tensors have to be ready on the model's stream."""
+        picked: (tokens int32 [B], log of each token's share).  The tensors have to be ready on the model's stream, and the results are
+        written there: another stream waits for it before it reads them."""
         B = uniforms.shape[0]
-        if next_dev is None:
-            next_dev = torch.empty(B, dtype=torch.int32, device=self.device)
-        logprobs = torch.empty(B, dtype=torch.float32, device=self.device)
+        given = (uniforms, temperature, top_k, top_p, min_p, next_dev)
         _refuse(uniforms=(uniforms, _F32, (B,)), temperature=(temperature, _F32, (B,)), top_k=(top_k, _I32, (B,)), top_p=(top_p, _F32, (B,)),
                 min_p=(min_p, _F32, (B,)), next_dev=(next_dev, _I32, (B,)))
-        _stream(self.device.index, (uniforms, temperature, top_k, top_p, min_p, next_dev))
+        _stream(self.device.index, given)
+        if next_dev is None:
+            next_dev = self._empty(B, dtype=_I32)
+        logprobs = self._empty(B, dtype=_F32)
+        if self._elsewhere():
+            for t in given:
+                if t is not None:  # the caller may drop it before the model's stream has read or written it
+                    t.record_stream(self._own_stream())
         self._check(self.L.dbt_sample_last(self._h, SAMPLING_FORMAT.pack(SAMPLING_FORMAT.size, 0, uniforms.data_ptr(), _p(temperature) or 0, _p(top_k) or 0,
                                                                          _p(top_p) or 0, _p(min_p) or 0), B, next_dev.data_ptr(), logprobs.data_ptr()))
         return next_dev, logprobs

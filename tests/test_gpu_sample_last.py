@@ -152,6 +152,43 @@ def test_sampled_decoding_feeds_itself_and_leaves_the_cache_as_greedy_steps_do()
     assert len({int(t[0]) for t in fed}) > 3
 
 
+@pytest.mark.parametrize("own", [True, False])
+def test_a_model_on_another_stream_than_the_callers(own):
+    """The model on a stream of its own and the caller on the default one, or the other way round.  While the model's stream is still
+    busy, memory of a dropped result or input goes to nobody who works on the caller's stream, and all results are those of one stream."""
+    cfg, B = CONFIGS["bf16"], 4
+    side = torch.cuda.Stream()
+    weights = binding.weights_to_device(make_weights(cfg, seed=0, matrix_std=0.08), "cuda:0")
+    tok = make_tokens(cfg, B, 9, seed=9).cuda()
+    u, p = torch.rand(B, generator=torch.Generator().manual_seed(10)), torch.full((B,), 0.9)
+    plain = binding.Model(cfg, weights, B, 64)
+    logits, first = plain.prefill(tok[:, :4].contiguous(), want_logits=True), plain.prefill_boundary(tok[:, 4:].contiguous())
+    want = plain.sample_last(u.cuda(), top_p=p.cuda())
+    m = binding.Model(cfg, weights, B, 64, stream=side if own else None)
+    models, callers = (side, torch.cuda.default_stream()) if own else (torch.cuda.default_stream(), side)
+    with torch.cuda.stream(callers):
+        a, b = tok[:, :4].contiguous(), tok[:, 4:].contiguous()
+        torch.cuda.synchronize()
+        got_logits, got = m.prefill(a, want_logits=True), m.prefill_boundary(b)
+        du, dp = u.cuda(), p.cuda()
+        torch.cuda.synchronize()
+        with torch.cuda.stream(models):
+            torch.cuda._sleep(200_000_000)  # a tenth of a second
+        busy = torch.cuda.Event()
+        tokens, logp = m.sample_last(du, top_p=dp)
+        busy.record(models)
+        gone = {x.data_ptr() for x in (logp, du, dp)}
+        del logp, du, dp
+        others = [torch.full((B,), 7.0, device="cuda") for _ in range(600)]
+        assert not busy.query()  # the sampler has yet to run
+        assert not gone & {x.data_ptr() for x in others}
+        kept, logp = m.sample_last(u.cuda(non_blocking=False), top_p=p.cuda())
+        torch.cuda.synchronize()
+        assert all((x == 7.0).all() for x in others)
+        for x, y in ((tokens, want[0]), (kept, want[0]), (logp, want[1]), (got_logits, logits), *((got[k], first[k]) for k in first)):
+            assert torch.equal(x, y)
+
+
 def test_refusals():
     cfg, B = CONFIGS["fp32"], 2
     m = model(cfg, B)
