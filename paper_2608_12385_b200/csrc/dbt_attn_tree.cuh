@@ -10,8 +10,9 @@
 // unnormalised output with its maximum and sum in the workspace, and a second kernel joins them in the order of the keys (no
 // atomics: results do not depend on timing).  Lengths are read on the device, so a captured call serves later lengths.
 //
-// Measured, bf16, head dimension 128: 16 sequences of up to 2048 keys and 16 nodes, 16 heads over 8 (74 MB of keys and values) 35 us,
-// 2.1 TB/s; 4 sequences of 32768 keys and 64 nodes, 32 heads over 8 (541 MB, 137 GFLOP) 156 us, 3.5 TB/s and 0.88 PFLOP/s.
+// Measured, bf16, head dimension 128, a call with both kernels: 16 sequences of up to 2048 keys and 16 nodes, 16 heads over 8 (74 MB of
+// keys and values) 35 us, 2.1 TB/s; 4 sequences of 32768 keys and 64 nodes, 32 heads over 8 (541 MB, 137 GFLOP) 175 to 184 us, 2.9 to 3.1 TB/s
+// and 0.75 to 0.78 PFLOP/s, of which 156 us (3.5 TB/s, 0.88 PFLOP/s) are the first kernel's.
 #pragma once
 
 #include "dbt_ptx.cuh"
@@ -346,7 +347,7 @@ __global__ void __launch_bounds__(256, TreeSimtCfg<D, RM>::kBlocksPerSm) attn_tr
 // exponentials a cycle; tensor-memory and shared-memory traffic the rest) and 1640 in which it waits for its products (1200 of the
 // tensor pipe, and the signals).  HBM would take 2150, and loads taken out save 4 %.  128 rows or fewer and ragged lengths: what a run
 // costs besides its tiles, of 67k cycles 4k to find its place, 4k for the first queries, 12k for joining the groups and writing.
-// Not better: scores of 64 keys in two buffers (240 us where this takes 156: products 64 wide take as long as 128 wide),
+// Not better: scores of 64 keys in two buffers (240 us where this form took 156: products 64 wide take as long as 128 wide),
 // 16 softmax warps with half a row a thread (176), a quarter of the exponentials as polynomials on the multiply-add pipes
 // (173: registers), scores read in pieces of 32 twice (169).
 //

@@ -880,7 +880,8 @@ __global__ void moe_lists_kernel(const int32_t *idx, int R, int kmax, int E, int
 // Scores that the tokens of a step are drawn by: log(alpha p + (1 - alpha) mean_j q_j) (Eq. alpha, Eq. mixloss; Appendix C.1) from the
 // records of readout_stats_kernel, a CTA per (row, chunk).  A sampler's temperature then acts on the mixture itself.  Formed from the paths'
 // logarithms, x_j = z_j - m_j - log d_j + log of the path's share, as max x + log sum e^(x_j - max x): as a probability a token 104 below the
-// largest would be 0 in fp32, and one 87 below a few bits, while a high temperature gives such tokens most of the mass.
+// largest would be 0 in fp32, and one 87 below a few bits, while a high temperature gives such tokens most of the mass.  A sampled step's token with the records made anew, by a call of
+// 32 rows of 128256 with two paths: 62 us (19 of them the sampler's; 60 with the probabilities), 16 rows of 32000: 27 us.
 __global__ void __launch_bounds__(kRoThreads) mix_scores_kernel(const float *Z, int B, int V, int chunk, int P, const float *stats, float *scores) {
     pdl_enter();
     __shared__ float top[1 + kMaxBranches], shift[1 + kMaxBranches];  // per path m_j; the path's share and normaliser as a logarithm

@@ -120,7 +120,8 @@ bool strides_fit(const int64_t *s, int n, int dtype) {
 
 // ---- tree attention ----------------------------------------------------------------------------------------------
 // An item costs about as much as five (fp32: one) of its tiles besides them: 16 ragged sequences 63 us without, 42 us with four to six
-// (then), 37, 36, 39 us with three, five, eight (now); long items do not care.
+// (then), 37, 36, 39 us with three, five, eight (now); long items do not care.  Measured with head dimension 128 and up to 128 rows a key;
+// 64 and 256 rows take the same number unmeasured.
 constexpr int kTreeLead = 5;
 struct TreeShape {
     int rows, keys, blocks, per_sm, lead;
@@ -130,7 +131,8 @@ long long tree_units(const dbt_attn_tree_args &a) {
     const int rows = a.max_nodes * (a.n_q_heads / a.n_kv_heads), keys = a.dtype == DBT_DTYPE_BF16 ? 128 : kTsKeys;
     return ((long long)a.pages_per_seq * 16 / keys + 1 + kTreeLead) * ((rows + 15) / 16) * a.n_kv_heads * a.B;
 }
-// Blocks: as many as the device holds at once, no more than there can be tiles.
+// Blocks: one for each SM, two of the fp32 form for 16 rows (the one for 64 rows of 64 elements would fit twice as well; one was not held
+// against two), no more than there can be tiles.
 TreeShape tree_shape(const dbt_attn_tree_args &a) {
     TreeShape s;
     const int G = a.n_q_heads / a.n_kv_heads, rows = a.max_nodes * G;
@@ -388,7 +390,8 @@ dbt_status dbt_op_sample(const void *logits, int32_t dtype, int32_t rows, int32_
     // Blocks per row: enough to fill the device (four are resident per SM), or two per SM where a block's share is short already;
     // and no more than leave a block 4096 values.  256 rows of 128256, top-k 50 with top-p and min-p: 69 us with 8 blocks a row, 56 with 4;
     // top-k 400: 109, 78; without filters 90, 88; settings of all kinds 118, 127.  256 rows of 32000, the same filters: 72, 34, 24 us with 8,
-    // 4, 2 (then; 21 now); one row of 128256 without filters: 25, 42, 73 with 8, 4, 2 (then; 13 now).
+    // 4, 2 (then; 21 now); one row of 128256 without filters: 25, 42, 73 with 8, 4, 2 (then; 13 now).  Between and
+    // beyond these sizes the rule is a guess.
     const long long sms = sm_count();
     int cluster = 1;
     while (vocab > cluster * kSmMaxSlice ||

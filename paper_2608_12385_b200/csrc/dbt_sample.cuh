@@ -34,7 +34,7 @@
 // What bounds it: one row, the cluster barriers (one to two microseconds each); many rows, where all of a row's exponentials are
 // needed (top-p alone, no filter at all), the latency of the 64-bit chains and of the passes over L2, else the passes.  Measured,
 // fp32 logits, 128256 a row: one row 13 us without filters, 15 with top-k 50, top-p and min-p, 23 with top-p alone; 256 rows (131 MB, 20 us
-// of HBM) 88, 56 and 137 to 191, with settings of all kinds 125 to 129; 64 rows without filters 28.
+// of HBM) 89, 57 and 137 to 193, with settings of all kinds 126 to 132; 64 rows without filters 28.
 #pragma once
 
 #include <type_traits>
@@ -49,7 +49,7 @@ constexpr int kSmList = 1024;    // values that one block sorts
 constexpr int kSmGuess = 512;    // the largest top_k of the short way
 // Values that the short way asks for where top-p alone says how many: a list of up to 512 is sorted in two thirds of the time that one
 // of up to 1024 takes.  With 512, 384, 256: one row of 32000 21.0, 19.0, 18.9 us; 64 rows of 128256 114, 85, 83; 256 rows whose
-// border lies below the list 295, 294, 383 (too few exact ones for the middle way).
+// border lies below the list 295, 294, 383 (too few exact ones for the middle way).  Not measured at other widths.
 constexpr int kSmNucleus = 384;
 constexpr int kSmMaxBuckets = 64;  // for the threads' maxima
 constexpr int kSmRun = 256;      // ids summed together by a warp on the long way
@@ -1151,9 +1151,10 @@ __global__ void __launch_bounds__(NT, NT == 256 ? 4 : 1) sample_kernel(const Sam
             });
             bounded = bracket(std::false_type{}, goal, border);
         }
-        if (bounded) {
-        } else if (narrow(std::false_type{}, goal, false, nullptr, range, border) == 1) listed = true;
-        else bounded = true;
+        if (!bounded) {
+            listed = narrow(std::false_type{}, goal, false, nullptr, range, border) == 1;
+            bounded = !listed;
+        }
     }
     if (!listed && f.p_on) {
         SampleBorder other;
@@ -1163,15 +1164,15 @@ __global__ void __launch_bounds__(NT, NT == 256 ? 4 : 1) sample_kernel(const Sam
             border = other;
             bounded = true;
         } else {
-        const int how = narrow(std::true_type{}, goal, !known.on, bounded ? &border : nullptr, range, other);
-        goal_known = true;
-        if (how == 1) {
-            listed = true;
-        } else {
-            if (bounded && other.tau == border.tau) other.ties = min(other.ties, border.ties);
-            border = other;  // (never below top-k's: masses were counted inside it)
-            bounded = true;
-        }
+            const int how = narrow(std::true_type{}, goal, !known.on, bounded ? &border : nullptr, range, other);
+            goal_known = true;
+            if (how == 1) {
+                listed = true;
+            } else {
+                if (bounded && other.tau == border.tau) other.ties = min(other.ties, border.ties);
+                border = other;  // (never below top-k's: masses were counted inside it)
+                bounded = true;
+            }
         }
     }
     if (listed) {
