@@ -480,7 +480,8 @@ def _p(t):
 
 class Model:
     """A Decode-Branch model handle: owns (as torch tensors) the KV pool and the workspace
-    the library borrows, and keeps the device weights alive."""
+    the library borrows, and keeps the device weights alive.  Calls enqueue their work on `stream` (None: the default
+    stream) and their results are written there; a caller on another stream waits for it before reading them."""
 
     def __init__(self, cfg: ModelConfig, weights_dev: dict, max_batch: int, max_seq: int,
                  num_pages: int | None = None, stream: torch.cuda.Stream | None = None):

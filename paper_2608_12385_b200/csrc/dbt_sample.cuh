@@ -265,7 +265,7 @@ __device__ __forceinline__ bool sm_round(SampleRow<T, NT> &row, SampleRange &r, 
         for (int e = 0; e < 4; e++) {
             const uint32_t k = sm_key(z[e]);
             const bool in = e < m && k <= r.hi && k >= lo;
-            b[e] = in ? min((int)((r.hi - k) >> shift), NB - 1) : -1;
+            b[e] = in ? (int)min((r.hi - k) >> shift, (uint32_t)(NB - 1)) : -1;  // (patterns may be more than 2^31 apart)
             const unsigned long long one = in ? 1ull << (8 * (b[e] & 7)) : 0ull;
             if (NB <= 8 || b[e] < 8) c0 += one;
             else c1 += one;

@@ -529,6 +529,28 @@ def test_sample_clusters_whose_blocks_begin_at_different_times(V, R):
         assert torch.equal(binding.op_sample(*args)[0], expected)
 
 
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("V", [1500, 2207, 40000, 128256])
+def test_sample_windows_of_a_few_neighbouring_numbers(dtype, V):
+    """Logits so large, or temperatures so low, that the first window of a search holds fewer numbers than it has buckets, while others lie
+    more than 2^31 ordered patterns below."""
+    g = gen(V)
+    z = torch.randn(6, V, generator=g) * torch.tensor([1e6, 1e7, 1e8, 1e12, 3e36, 1e7])[:, None]
+    z[5, V // 3 : V // 3 + 1200] = 4e7
+    z = z.to(TYPES[dtype])
+    u = torch.rand(6, generator=g).tolist()
+    for t in (1.0, 1e7, 1e30, 1e37):
+        check_sample(z, u, temperature=[t] * 6, top_k=[V - 1, V - 5, V // 2 + 300, 3 * V // 4, V - 2, 1300])
+        check_sample(z, u, temperature=[t] * 6, top_k=[V - 1, V - 5, V // 2 + 300, 3 * V // 4, V - 2, 1300], top_p=[0.3, 0.9, 0.5, 0.999, 0.8, 0.7])
+        check_sample(z, u, temperature=[t] * 6, top_p=[0.3, 0.9, 0.5, 0.999, 0.8, 0.7])
+    y = torch.randn(6, V, generator=g) * 3
+    y[:, 100 : 100 + V * 2 // 3] = torch.tensor([4.0, 8.0, 12.0, 16.0, 0.5, 100.0])[:, None]
+    y = y.clamp(max=y[:, 100:101]).to(TYPES[dtype])
+    for t in (1e-4, 1e-6, 1e-7, 1e-12, 1e-40):
+        for kw in (dict(top_p=[0.5, 0.25, 0.75, 0.9, 0.1, 0.6]), dict(top_k=[V - 1, V // 2, 600, 1025, V // 3, 2], top_p=[0.5, 0.25, 0.75, 0.9, 0.1, 0.6]), dict(top_k=[V - 1, V // 2, 600, 1025, V // 3, 2])):
+            check_sample(y, u, temperature=[t] * 6, **kw)
+
+
 def test_sample_strided_and_odd_rows():
     g = gen(21)
     store = torch.randn(5, 1003, generator=g) * 2
