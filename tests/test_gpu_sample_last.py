@@ -170,10 +170,10 @@ def test_a_model_on_another_stream_than_the_callers(own):
         a, b = tok[:, :4].contiguous(), tok[:, 4:].contiguous()
         torch.cuda.synchronize()
         got_logits, got = m.prefill(a, want_logits=True), m.prefill_boundary(b)
-        du, dp = u.cuda(), p.cuda()
+        du, dp, _ = u.cuda(), p.cuda(), torch.full((B,), 7.0, device="cuda")
         torch.cuda.synchronize()
         with torch.cuda.stream(models):
-            torch.cuda._sleep(200_000_000)  # a tenth of a second
+            torch.cuda._sleep(600_000_000)  # a third of a second
         busy = torch.cuda.Event()
         tokens, logp = m.sample_last(du, top_p=dp)
         busy.record(models)
